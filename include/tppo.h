@@ -452,6 +452,148 @@ int tppo_value_head(const void* hidden, int64_t n_rows, int64_t H, int64_t ld_hi
                     float* v_out, int32_t* status, void* stream);
 
 /* ---------------------------------------------------------------------------
+ * tppo_layer_norm -- the trunk's last norm, on the rows that the heads project:
+ * between the packed hidden states of the last block and tppo_token_logprobs /
+ * tppo_value_head.  For token m with row r = rows[m]:
+ *   mean[m] = sum_h x[r, h] / H
+ *   rstd[m] = 1 / sqrt(sum_h (x[r, h] - mean[m])^2 / H + eps)
+ *   y[m, h] = (x[r, h] - mean[m]) * rstd[m] * weight[h] + bias[h]
+ * in fp32, rounded once.  y is compact: the heads take it with rows 0 .. M-1.
+ *
+ * in : x [n_rows, H] of type dt, row stride ld_x; weight[H], bias[H] of type
+ *      dt_w (fp32, or bf16 with bf16 x; bias may be NULL: 0); rows[M] int32 (NULL: rows 0 .. M-1; the same
+ *      row may come several times); m_actual as in tppo_token_logprobs.
+ *      1 <= H <= 16384, any strides >= H and any base address that the type allows.
+ * out: y [M, H] of type dt, row stride ld_y; mean[M], rstd[M] fp32 (each may be
+ *      NULL), what tppo_layer_norm_backward takes.  Rows from m_actual on are
+ *      left as they were.  No output may overlap an input.
+ * A row index outside [0, n_rows) gives a row of NaN (and NaN statistics) and
+ * sets TPPO_STATUS_BAD_ROW.
+ * Errors: sizes -> TPPO_ERR_SIZE, eps negative or not finite or a pointer off
+ *      its type's alignment -> TPPO_ERR_PARAM, unknown types -> TPPO_ERR_DTYPE.
+ */
+int tppo_layer_norm(const void* x, int64_t n_rows, int64_t H, int64_t ld_x, tppo_dtype dt,
+                    const void* weight, const void* bias, tppo_dtype dt_w, float eps,
+                    const int32_t* rows, int64_t M, const int64_t* m_actual,
+                    void* y, int64_t ld_y, float* mean, float* rstd, int32_t* status, void* stream);
+
+/* ---------------------------------------------------------------------------
+ * tppo_layer_norm_backward -- its derivatives.  With xh = (x[r] - mean) * rstd
+ * and g = grad_y[m] * weight, for every token:
+ *   grad_x[m, h]    = rstd * (g_h - sum g / H - xh_h * sum(g * xh) / H)
+ *   grad_weight[h] (+)= sum_m grad_y[m, h] * xh[m, h]
+ *   grad_bias[h]   (+)= sum_m grad_y[m, h]
+ * in fp32; the sums over the tokens are taken in a fixed order (the same call
+ * gives the same bits).
+ *
+ * in : grad_y [M, H] of type dt_gy, row stride ld_gy (grad_hidden of
+ *      tppo_token_logprobs_backward is one, in fp32); x, weight, rows, M,
+ *      m_actual as in the forward call; mean, rstd what it returned.
+ * out: grad_x of type dt_gx, row stride ld_gx: token m's row is
+ *      out_index[m] (out_index NULL: row m) of n_out rows; rows that no token
+ *      has are left as they were.  The entries of out_index must be distinct.
+ *      grad_weight[H], grad_bias[H] fp32, overwritten, or added to when
+ *      accumulate_w != 0.  Each of the three may be NULL = not wanted.
+ *      fp32 x goes with fp32 grad_y and grad_x; bf16 x with either type in both.
+ * A row index outside [0, n_rows) gives a grad_x row of NaN, adds nothing to
+ * the weights' derivatives and sets TPPO_STATUS_BAD_ROW, which an out_index
+ * outside [0, n_out) sets as well (that row is not written).
+ * workspace: tppo_layer_norm_backward_workspace_bytes(M, H); not needed (may be
+ *      NULL) where neither grad_weight nor grad_bias is wanted.
+ */
+size_t tppo_layer_norm_backward_workspace_bytes(int64_t M, int64_t H);
+int tppo_layer_norm_backward(const void* grad_y, int64_t ld_gy, tppo_dtype dt_gy,
+                             const void* x, int64_t n_rows, int64_t H, int64_t ld_x, tppo_dtype dt,
+                             const void* weight, tppo_dtype dt_w, const float* mean, const float* rstd,
+                             const int32_t* rows, int64_t M, const int64_t* m_actual,
+                             void* grad_x, int64_t ld_gx, tppo_dtype dt_gx, const int32_t* out_index, int64_t n_out,
+                             float* grad_weight, float* grad_bias, int32_t accumulate_w,
+                             void* workspace, size_t workspace_bytes, int32_t* status, void* stream);
+
+/* ---------------------------------------------------------------------------
+ * tppo_balance_loss -- the auxiliary loss that keeps the experts of a
+ * mixture-of-experts policy evenly used, over the same tokens as the policy
+ * loss, with the per-expert counts.  For token m with row r = rows[m], of N:
+ *   p[m, e]      = exp(logits[r, e]) / sum_e' exp(logits[r, e'])
+ *   counts[e]    = number of (m, j), j < k, with experts[r, j] = e
+ *   mean_prob[e] = sum_m p[m, e] / N
+ *   loss         = coefficient * E * sum_e counts[e] / (k N) * mean_prob[e]
+ * An even use of all experts gives loss = coefficient.  N = 0 gives zeros.
+ *
+ * in : logits [n_rows, E] of type dt, row stride ld; experts [n_rows, k] int32,
+ *      row stride ld_experts: the experts that the router chose, -1 where it
+ *      chose none (a token that found its expert full); rows, M, m_actual as in
+ *      tppo_layer_norm.  1 <= E <= 2048, 1 <= k <= 1024, M < 2^31,
+ *      M k <= 2^36.
+ *      A logit of -inf is an expert that cannot be chosen (p = 0); a row that
+ *      has nothing else has p = 0 throughout, and still counts among the N.
+ *      NaN and +inf give NaN.
+ * out: loss fp32, counts[E] int64, mean_prob[E] fp32 (each may be NULL).
+ * A row outside [0, n_rows) counts among the N, adds nothing and sets
+ * TPPO_STATUS_BAD_ROW; an expert outside [-1, E) is not counted and sets
+ * TPPO_STATUS_BAD_TARGET.  Sums are taken in a fixed order.
+ * workspace: tppo_balance_loss_workspace_bytes(M, E), for both calls.
+ */
+size_t tppo_balance_loss_workspace_bytes(int64_t M, int64_t E);
+int tppo_balance_loss(const void* logits, int64_t n_rows, int64_t E, int64_t ld, tppo_dtype dt,
+                      const int32_t* experts, int64_t k, int64_t ld_experts,
+                      const int32_t* rows, int64_t M, const int64_t* m_actual, float coefficient,
+                      float* loss, int64_t* counts, float* mean_prob,
+                      void* workspace, size_t workspace_bytes, int32_t* status, void* stream);
+
+/* ---------------------------------------------------------------------------
+ * tppo_balance_loss_backward -- its derivative with respect to the logits, the
+ * counts being constants, and the loss, counts and means with it:
+ *   grad_logits[m, i] = scale * coefficient * E / N * p[m, i] * (f_i - sum_e f_e p[m, e]),
+ *   f_e = counts[e] / (k N).
+ * For a batch spread over several calls or devices, counts_in[E] (device int64,
+ * the counts of all of it) and token_denominator (> 0, its number of tokens)
+ * replace this call's own in f and N -- the loss and mean_prob of the calls
+ * then add up to the whole batch's -- while `counts` stays this call's.
+ * in : as tppo_balance_loss; scale finite; counts_in may be NULL.
+ * out: grad_logits of type dt, row stride ld_grad; rows by out_index and n_out
+ *      as in tppo_layer_norm_backward.  A row of only -inf gets 0, a row outside
+ *      [0, n_rows) NaN.
+ */
+int tppo_balance_loss_backward(const void* logits, int64_t n_rows, int64_t E, int64_t ld, tppo_dtype dt,
+                               const int32_t* experts, int64_t k, int64_t ld_experts,
+                               const int32_t* rows, int64_t M, const int64_t* m_actual, float coefficient,
+                               float scale, const int64_t* counts_in, int64_t token_denominator,
+                               void* grad_logits, int64_t ld_grad, const int32_t* out_index, int64_t n_out,
+                               float* loss, int64_t* counts, float* mean_prob,
+                               void* workspace, size_t workspace_bytes, int32_t* status, void* stream);
+
+/* ---------------------------------------------------------------------------
+ * tppo_orthogonalize -- an update (a weight matrix's gradient or momentum) made
+ * nearly orthogonal by Newton-Schulz products, what the Muon optimiser applies
+ * to hidden matrices.  For each of `count` matrices G, with X the wide one of G
+ * and its transpose:
+ *   X = G / (|G|_F + eps)
+ *   `steps` times:  A = X X^T;  X = a X + (b A + c A^2) X
+ *   out = scale * X, transposed back, rounded to bf16.
+ * With (a, b, c) = (3.4445, -4.7750, 2.0315) and 5 steps, singular values from
+ * 0.3 % of |G|_F on come to lie between 0.68 and 1.21.
+ * X is held to 22 bits, the operands of the products to 11 (fp16, scaled by
+ * powers of two), to 22 where rows or cols < 512, the diagonals of A and
+ * b A + c A^2 and all sums in fp32.
+ *
+ * in : g: `count` matrices [rows, cols] of type dt, row stride ld_g, stride_g
+ *      elements from one to the next; 1 <= rows, cols <= 65536, 0 <= steps <= 64;
+ *      a, b, c, eps, scale finite, eps >= 0.
+ * out: out: `count` matrices [rows, cols] bf16, row stride ld_out, stride_out
+ *      apart; no overlap with g or each other.
+ * A matrix of zeros stays zero (with eps > 0); one with a NaN or an infinity
+ * gives NaN.  Coefficients under which the iteration grows without bound end in
+ * infinities and NaN.
+ * workspace: tppo_orthogonalize_workspace_bytes(count, rows, cols).
+ */
+size_t tppo_orthogonalize_workspace_bytes(int64_t count, int64_t rows, int64_t cols);
+int tppo_orthogonalize(const void* g, int64_t count, int64_t rows, int64_t cols, int64_t ld_g, int64_t stride_g,
+                       tppo_dtype dt, int32_t steps, float a, float b, float c, float eps, float scale,
+                       void* out, int64_t ld_out, int64_t stride_out,
+                       void* workspace, size_t workspace_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------
  * tppo_diag_mfma_rate -- a measuring stick, not a step of the method: runs the
  * inner loop of the LM-head kernel (v_mfma_f32_16x16x32_bf16, 8 wavefronts per
  * workgroup, one workgroup per CU, 32 MFMAs per wavefront and iteration) on

@@ -1,0 +1,544 @@
+// tppo_orthogonalize: Newton-Schulz products that drive the singular values of an update to one another.
+//     X = G / (|G|_F + eps), wide;   steps times:  A = X X^T,  B = b A + c A A,  X = a X + B X
+// Three matrix products a step on the matrix cores, 2 m (m n + m m + m n) flop, of which the first two have symmetric results: only the
+// tiles on and below the diagonal are computed, and written twice.
+//
+// Precision.  A rounding of X is a matrix with singular values in every direction, and the iteration multiplies small ones by up to a
+// each time, a^steps = 485 in all: bf16 operands turn a gradient of rank one into noise (error 1.2 of 1), fp16 ones still 0.15.  So
+//   X     is a pair of fp16, hi + lo / 2048, 22 bits, and a X is taken from both; the product B X takes hi alone: what that loses lies in
+//         the range of B, where the large singular values are, and is not amplified;
+//   A, B  have their diagonals, which tend to 1 and a - 1 .. in fp32 vectors, and only what is off the diagonal in fp16.
+// What is off the diagonal is small against it in large matrices only; where m < kSplitBelow, A and B are pairs as well, and a product
+// is hi hi + (hi lo + lo hi) / 2048, three passes over its contraction.  Against 64 bits, before the rounding to bf16 (1.7e-3), emulated:
+// one pass  m = 512 rank one 1.5e-3, full 7e-4;  256 2.3e-3;  64 9e-3;  three passes  1e-4 at most.
+// All scales are powers of two: X is held times S = 2^round(log2(n) / 2), so that entries are around one from the first step to the last,
+// A and B off the diagonal times 64.  Where |G|_F is so far below eps that X stays under 1/4 to the end, S is larger by as much.
+#include "head_tile.h"
+
+namespace tppo {
+
+typedef _Float16 half_t;
+typedef half_t half8 __attribute__((ext_vector_type(8)));
+typedef half_t half4 __attribute__((ext_vector_type(4)));
+
+constexpr float kLoScale = 2048.f, kOffScale = 64.f;
+constexpr int kSplitBelow = 512;
+
+enum NsMode { kGram, kPoly, kUpdate, kLast };        // A = X X^T;  B = b A + c A A;  X = a X + B X;  the same into the caller's array
+
+struct NsArgs {
+    // out tile [T rows][V columns]:  sum_k t_op[t, k] * v_op[v, k], or v_op[k, v] where that operand lies with K as its row
+    const half_t *t_op, *v_op;
+    int64_t ld_t, ld_v, each_t, each_v;              // in elements; from one matrix of the stack to the next
+    int64_t lo_t, lo_v;                              // bytes from an operand to its low halves
+    int n_t, n_v, k;                                 // rows of either side; contraction, a multiple of 64
+    int tiles_t, tiles_v, tiles;                     // tiles: of one matrix
+    // kGram: off, diag out;  kPoly: off, diag in, off_out, diag_out out;  kUpdate, kLast: diag (of B), hi, lo in, hi_out, lo_out / out out
+    half_t *off, *off_out, *off_lo, *off_out_lo, *hi, *lo, *hi_out, *lo_out;
+    float *diag, *diag_out;
+    int64_t each_off, each_diag, each_x;
+    int ld_off, ld_x;
+    const float2* scales;                            // by matrix: 1 / S^2, scale / S
+    float a, b, c;
+    uint16_t* out;                                   // kLast: bf16, times out_scale
+    int64_t ld_out, each_out;
+    int m, n, transposed;
+};
+
+template <int TV, int TT, int WV, int WT, bool KMAJOR, bool SPLIT>
+struct NsCfg {
+    static constexpr int kTileV = TV, kTileT = TT, kWavesV = WV, kWavesT = WT, kWaves = WV * WT, kThreads = kWaves * 64;
+    static constexpr int kBK = 64, kRowBytes = 128, kRows = TV + TT, kStageBytes = kRows * kRowBytes, kLdsBytes = 2 * kStageBytes;
+    static constexpr int kWaveV = TV / WV, kWaveT = TT / WT, kVB = kWaveV / 16, kTB = kWaveT / 16;
+    static constexpr int kDma = kStageBytes / 1024, kDmaPerWave = kDma / kWaves, kDmaV = TV * kRowBytes / 1024;
+    static constexpr int kSteps = 2 * kVB;           // of kTB MFMAs each
+    static constexpr int kSpreadSteps = kSteps / 2;  // a stage's transfers go out over so many
+    static constexpr bool kKMajor = KMAJOR, kSplit = SPLIT;
+    static constexpr int kKRowBytes = TV * 2;        // K-major: a stage is 64 rows of TV columns
+    static_assert(kDmaPerWave * kWaves == kDma && kDma * 1024 == kStageBytes, "whole transfers");
+    static_assert(!KMAJOR || TV % 128 == 0, "the swizzle of K-major rows spans 256 bytes");
+};
+
+__device__ __forceinline__ int ns_swz(int r) { return (r >> 1) & 7; }
+__device__ __forceinline__ int ns_swz_k(int k) { return ((k & 3) | ((k >> 3) & 1) << 2) << 1; }
+
+// Tile `id` of a matrix.  Rectangular: blocks of 8 T tiles, column by column, so that an XCD's workgroups share operands in its L2.
+// Symmetric: the same over v >= t.
+template <bool SYMMETRIC>
+__device__ __forceinline__ void ns_tile_at(int id, int tiles_t, int tiles_v, int& t, int& v) {
+    constexpr int kBlock = 8;
+    if constexpr (!SYMMETRIC) {
+        const int block = id / (kBlock * tiles_v), in = id - block * kBlock * tiles_v, height = min(kBlock, tiles_t - block * kBlock);
+        v = in / height;
+        t = block * kBlock + in - v * height;
+    } else {
+        int first = 0;
+        for (;;) {
+            const int height = min(kBlock, tiles_t - first), corner = height * (height + 1) / 2;
+            const int all = corner + (tiles_v - first - height) * height;
+            if (id < all) {
+                if (id < corner) {
+                    int col = 0;
+                    while ((col + 1) * (col + 2) / 2 <= id) ++col;
+                    v = first + col;
+                    t = first + id - col * (col + 1) / 2;
+                } else {
+                    const int col = (id - corner) / height;
+                    v = first + height + col;
+                    t = first + id - corner - col * height;
+                }
+                return;
+            }
+            id -= all;
+            first += kBlock;
+        }
+    }
+}
+
+template <class C, NsMode MODE>
+__global__ __launch_bounds__(C::kThreads, C::kLdsBytes <= 80 * 1024 ? C::kWaves / 2 : C::kWaves / 4) void ns_product_kernel(NsArgs p) {
+    constexpr bool kSymmetric = MODE == kGram || MODE == kPoly;
+    constexpr int kVB = C::kVB, kTB = C::kTB, kDmaPerWave = C::kDmaPerWave;
+    extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+    // workgroups go round-robin over the 8 XCDs: consecutive tiles to each (one more to the first gridDim.x % 8 of them)
+    const int xcd = (int)blockIdx.x & 7, id = xcd * ((int)gridDim.x >> 3) + min(xcd, (int)gridDim.x & 7) + ((int)blockIdx.x >> 3);
+    const int mat = id / p.tiles;
+    int tile_t, tile_v;
+    ns_tile_at<kSymmetric>(id - mat * p.tiles, p.tiles_t, p.tiles_v, tile_t, tile_v);
+    const int t0 = tile_t * C::kTileT, v0 = tile_v * C::kTileV;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int wv = wave / C::kWavesT, wt = wave % C::kWavesT, col = lane & 15, grp = lane >> 4;
+    const unsigned lds_base = (unsigned)(size_t)(__attribute__((address_space(3))) unsigned char*)smem;
+
+    // transfers: this wavefront's are kDmaPerWave of the stage's, the V side's first
+    const char* src[kDmaPerWave];
+    const char *t_base = reinterpret_cast<const char*>(p.t_op + mat * p.each_t), *v_base = reinterpret_cast<const char*>(p.v_op + mat * p.each_v);
+#pragma unroll
+    for (int q = 0; q < kDmaPerWave; ++q) {
+        const int d = wave * kDmaPerWave + q;
+        if (d < C::kDmaV && C::kKMajor) {
+            constexpr int kPerRow = C::kKRowBytes / 16;
+            const int at = d * 64 + lane, k = at / kPerRow, c = (at % kPerRow) ^ ns_swz_k(k);
+            src[q] = v_base + ((int64_t)k * p.ld_v + min(v0 + c * 8, p.n_v - 8)) * 2;
+        } else {
+            const int r = (d < C::kDmaV ? d : d - C::kDmaV) * 8 + (lane >> 3), staged = d * 8 + (lane >> 3);
+            const int chunk = ((lane & 7) ^ ns_swz(staged)) * 16;
+            if (d < C::kDmaV) src[q] = v_base + (int64_t)min(v0 + r, p.n_v - 1) * p.ld_v * 2 + chunk;
+            else src[q] = t_base + (int64_t)min(t0 + r, p.n_t - 1) * p.ld_t * 2 + chunk;
+        }
+    }
+    // (three passes: T's low halves, V's, neither's)
+    int64_t pos = C::kSplit ? p.lo_t : 0, pos_v = 0;
+    const int stages_once = p.k / C::kBK, stages = C::kSplit ? 3 * stages_once : stages_once;
+    int issued = 0;
+    const int64_t step_v = C::kKMajor ? (int64_t)C::kBK * p.ld_v * 2 : C::kRowBytes;
+    const unsigned dst0 = lds_base + wave * kDmaPerWave * 1024;
+    unsigned dst = dst0;
+    auto issue_one = [&](int q) {
+        const bool on_v = wave * kDmaPerWave + q < C::kDmaV;
+        const char* from = src[q] + (on_v ? pos_v : pos);
+        asm volatile("s_add_u32 m0, %0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off"
+                     :
+                     : "s"(dst), "v"(from), "i"(q * 1024)
+                     : "memory", "m0", "scc");
+    };
+    auto issue_advance = [&]() {
+        pos += C::kRowBytes;
+        pos_v += step_v;
+        dst = 2 * dst0 + C::kStageBytes - dst;
+        if constexpr (C::kSplit) {
+            if (++issued == stages_once) {
+                pos = 0;
+                pos_v = p.lo_v;
+            } else if (issued == 2 * stages_once) {
+                pos = pos_v = 0;
+            }
+        }
+    };
+    f32x4 acc[kVB][kTB] = {};
+    half8 fa[2], fb[2][kTB];
+    auto load_frags = [&](int stage, int step) {
+        const int k32 = step / kVB, vb = step % kVB, c = k32 * 4 + grp;
+        const unsigned char* st = smem + stage * C::kStageBytes;
+        if constexpr (C::kKMajor) {
+            typedef short s4 __attribute__((ext_vector_type(4)));
+            typedef __attribute__((address_space(3))) s4* lds_s4;
+            const int k = grp * 8 + (col >> 2), first = wv * kVB + vb;
+            const int lane_at = k * C::kKRowBytes + ((2 * first + ((col & 3) >> 1)) ^ ns_swz_k(k)) * 16 + (col & 1) * 8;
+            const unsigned from = lds_base + stage * C::kStageBytes + lane_at + k32 * 32 * C::kKRowBytes;
+            const s4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4)(size_t)from);
+            const s4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4)(size_t)(from + 4 * C::kKRowBytes));
+            fa[step & 1] = __builtin_bit_cast(half8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+        } else {
+            const int r = wv * C::kWaveV + vb * 16 + col;
+            fa[step & 1] = *reinterpret_cast<const half8*>(st + r * C::kRowBytes + ((c ^ ns_swz(r)) << 4));
+        }
+        if (vb == 0)
+#pragma unroll
+            for (int tb = 0; tb < kTB; ++tb) {
+                const int r = C::kTileV + wt * C::kWaveT + tb * 16 + col;
+                fb[k32][tb] = *reinterpret_cast<const half8*>(st + r * C::kRowBytes + ((c ^ ns_swz(r)) << 4));
+            }
+    };
+    // an MFMA step; this wavefront's transfers of the stage that was freed go out between those of the first kSpreadSteps
+    auto mfma_step = [&](int step, int part, bool on) {
+        const int k32 = step / kVB, vb = step % kVB;
+        constexpr int kSpread = C::kSpreadSteps * kTB;
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int tb = 0; tb < kTB; ++tb) {
+            acc[vb][tb] = __builtin_amdgcn_mfma_f32_16x16x32_f16(fa[step & 1], fb[k32][tb], acc[vb][tb], 0, 0, 0);
+            if (part < C::kSpreadSteps) {
+                if (on) {
+#pragma unroll
+                    for (int j = 0; j < kDmaPerWave; ++j)
+                        if (j * kSpread / kDmaPerWave == part * kTB + tb) issue_one(j);
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        }
+    };
+#pragma unroll
+    for (int q = 0; q < kDmaPerWave; ++q) issue_one(q);
+    issue_advance();
+    __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));
+    __syncthreads();
+    if (stages > 1) {
+#pragma unroll
+        for (int q = 0; q < kDmaPerWave; ++q) issue_one(q);
+        issue_advance();
+    }
+    load_frags(0, 0);
+    int stage = 0;
+    bool refill = false;
+    for (int it = 0; it < stages; ++it) {
+#pragma unroll
+        for (int ks = 0; ks + 1 < C::kSteps; ++ks) {
+            load_frags(stage, ks + 1);
+            mfma_step(ks, ks + 1, refill);
+            if (ks + 2 == C::kSpreadSteps && refill) issue_advance();
+        }
+        refill = false;
+        __builtin_amdgcn_s_waitcnt(kLgkm0);
+        if (it + 1 < stages) {
+            __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));
+            __syncthreads();
+            refill = it + 2 < stages;
+            load_frags(stage ^ 1, 0);
+        }
+        mfma_step(C::kSteps - 1, 0, refill);
+        stage ^= 1;
+        if constexpr (C::kSplit) {
+            if (it + 1 == 2 * stages_once) {
+#pragma unroll
+                for (int vb = 0; vb < kVB; ++vb)
+#pragma unroll
+                    for (int tb = 0; tb < kTB; ++tb) acc[vb][tb] *= 1.f / kLoScale;
+            }
+        }
+    }
+
+    // epilogue: a lane has four V columns in a row of T's, block by block
+    const float2 scales = p.scales[mat];
+#pragma unroll
+    for (int tb = 0; tb < kTB; ++tb) {
+        const int t = t0 + wt * C::kWaveT + tb * 16 + col;
+        if (t >= p.n_t) continue;
+#pragma unroll
+        for (int vb = 0; vb < kVB; ++vb) {
+            const int v = v0 + wv * C::kWaveV + vb * 16 + grp * 4;
+            if (v >= p.n_v) continue;
+            if constexpr (kSymmetric) {
+                half_t *out = (MODE == kGram ? p.off : p.off_out) + mat * p.each_off, *out_lo = nullptr;
+                if constexpr (C::kSplit) out_lo = (MODE == kGram ? p.off_lo : p.off_out_lo) + mat * p.each_off;
+                float* diag = (MODE == kGram ? p.diag : p.diag_out) + mat * p.each_diag;
+                const int64_t at = (int64_t)t * p.ld_off + v;
+                float x[4];
+                if constexpr (MODE == kGram) {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        x[e] = acc[vb][tb][e] * scales.x;
+                        if (v + e == t) diag[t] = x[e];
+                        x[e] *= kOffScale;
+                    }
+                } else {
+                    const half4 was = *reinterpret_cast<const half4*>(p.off + mat * p.each_off + at);
+                    half4 was_lo = {};
+                    if constexpr (C::kSplit) was_lo = *reinterpret_cast<const half4*>(p.off_lo + mat * p.each_off + at);
+                    const float* d = p.diag + mat * p.each_diag;
+                    const float dt = d[t];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const float w = C::kSplit ? fmaf((float)was_lo[e], 1.f / kLoScale, (float)was[e]) : (float)was[e], dv = d[v + e];
+                        if (v + e == t) diag[t] = fmaf(p.c, fmaf(acc[vb][tb][e], 1.f / (kOffScale * kOffScale), dt * dt), p.b * dt);
+                        x[e] = fmaf(p.c, fmaf(dt + dv, w, acc[vb][tb][e] * (1.f / kOffScale)), p.b * w);
+                    }
+                }
+                half4 o, o_lo;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    x[e] = v + e == t ? 0.f : x[e];
+                    o[e] = (half_t)x[e];
+                    o_lo[e] = (half_t)((x[e] - (float)o[e]) * kLoScale);
+                }
+                *reinterpret_cast<half4*>(out + at) = o;
+                if constexpr (C::kSplit) *reinterpret_cast<half4*>(out_lo + at) = o_lo;
+                if (tile_t != tile_v)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        out[(int64_t)(v + e) * p.ld_off + t] = o[e];
+                        if constexpr (C::kSplit) out_lo[(int64_t)(v + e) * p.ld_off + t] = o_lo[e];
+                    }
+            } else {
+                const int64_t at = mat * p.each_x + (int64_t)t * p.ld_x + v;
+                const half4 hi = *reinterpret_cast<const half4*>(p.hi + at), lo = *reinterpret_cast<const half4*>(p.lo + at);
+                const float lead = p.a + p.diag[mat * p.each_diag + t];
+                half4 new_hi, new_lo;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float x = fmaf(lead, fmaf((float)lo[e], 1.f / kLoScale, (float)hi[e]), acc[vb][tb][e] * (1.f / kOffScale));
+                    if constexpr (MODE == kUpdate) {
+                        new_hi[e] = (half_t)x;
+                        new_lo[e] = (half_t)((x - (float)new_hi[e]) * kLoScale);
+                    } else if (t < p.m && v + e < p.n) {
+                        const int64_t to = p.transposed ? (int64_t)(v + e) * p.ld_out + t : (int64_t)t * p.ld_out + v + e;
+                        p.out[mat * p.each_out + to] = (uint16_t)__builtin_bit_cast(uint16_t, (__bf16)(x * scales.y));
+                    }
+                }
+                if constexpr (MODE == kUpdate) {
+                    *reinterpret_cast<half4*>(p.hi_out + at) = new_hi;
+                    *reinterpret_cast<half4*>(p.lo_out + at) = new_lo;
+                }
+            }
+        }
+    }
+}
+
+// ---- |G|_F and the first X
+constexpr int kNsThreads = 256, kNsParts = 64;       // partial sums of squares a matrix
+template <class T>
+__device__ __forceinline__ float ns_value(const T* p) {
+    if constexpr (sizeof(T) == 4) return *p;
+    else return __uint_as_float((uint32_t)*p << 16);
+}
+__device__ __forceinline__ double ns_workgroup_sum(double x, double* place) {
+    x = wave_prefix(x);
+    if ((threadIdx.x & 63) == 63) place[threadIdx.x >> 6] = x;
+    __syncthreads();
+    x = 0.0;
+#pragma unroll
+    for (int w = 0; w < kNsThreads / kWave; ++w) x += place[w];
+    return x;
+}
+// (in 64 bits: squares of large fp32 values overflow, and nothing here is bound by arithmetic)
+template <class T>
+__global__ __launch_bounds__(kNsThreads) void ns_norm_kernel(const T* g, int rows, int cols, int64_t ld, int64_t each, double* parts) {
+    __shared__ double place[kNsThreads / kWave];
+    const T* from = g + blockIdx.y * each;
+    double sum = 0.0;
+    for (int r = blockIdx.x; r < rows; r += gridDim.x)
+        for (int c = threadIdx.x; c < cols; c += kNsThreads) {
+            const double x = (double)ns_value(from + (int64_t)r * ld + c);
+            sum = fma(x, x, sum);
+        }
+    sum = ns_workgroup_sum(sum, place);
+    if (threadIdx.x == 0) parts[(int64_t)blockIdx.y * kNsParts + blockIdx.x] = sum;
+}
+
+// X [mp, np], zeros beyond m x n, from G or its transpose, in tiles of 64 x 64 through LDS.  hi == NULL: no products follow, X times
+// out_scale goes to the caller's array.
+template <class T>
+__global__ __launch_bounds__(kNsThreads) void ns_begin_kernel(const T* g, int64_t ld, int64_t each, const double* parts, int count_parts,
+                                                              float eps, float scale, float s_scale, double growth, half_t* hi, half_t* lo,
+                                                              float2* scales, int mp, int np, int m, int n, int transposed,
+                                                              uint16_t* out, int64_t ld_out, int64_t each_out) {
+    __shared__ double place[kNsThreads / kWave];
+    __shared__ float tile[64][65];
+    const int mat = blockIdx.z;
+    double sum = 0.0;
+    if ((int)threadIdx.x < count_parts) sum = parts[(int64_t)mat * kNsParts + threadIdx.x];
+    sum = ns_workgroup_sum(sum, place);
+    const double norm = sqrt(sum) + (double)eps;
+    // (one of zeros with eps = 0 gives NaN, as 0 / 0 does; an infinity in G makes all of it NaN)
+    // growth: what the steps make of small singular values
+    const double most = sqrt(sum) / norm * growth;
+    const double lift = hi && most > 0.0 && most < 0.25 ? ldexp(1.0, -ilogb(most) - 3) : 1.0;
+    const double s_all = hi ? (double)s_scale * lift : (double)scale;
+    const double by = norm < 1.0e300 ? s_all / norm : __builtin_nan("");
+    if (hi && threadIdx.x == 0 && blockIdx.x == 0 && blockIdx.y == 0)
+        scales[mat] = make_float2((float)(1.0 / (s_all * s_all)), (float)((double)scale / s_all));
+    const T* from = g + mat * each;
+    const int i0 = blockIdx.y * 64, j0 = blockIdx.x * 64, lane = threadIdx.x & 63, part = threadIdx.x >> 6;
+    if (transposed) {                                // G is [n, m]
+        for (int r = part; r < 64; r += 4) tile[lane][r] = j0 + r < n && i0 + lane < m ? ns_value(from + (int64_t)(j0 + r) * ld + i0 + lane) : 0.f;
+    } else {
+        for (int r = part; r < 64; r += 4) tile[r][lane] = i0 + r < m && j0 + lane < n ? ns_value(from + (int64_t)(i0 + r) * ld + j0 + lane) : 0.f;
+    }
+    __syncthreads();
+    for (int r = part; r < 64; r += 4) {
+        const bool there = i0 + r < m && j0 + lane < n;
+        const float x = there ? (float)((double)tile[r][lane] * by) : 0.f;
+        if (hi) {
+            const int64_t at = ((int64_t)mat * mp + i0 + r) * np + j0 + lane;
+            const half_t h = (half_t)x;
+            hi[at] = h;
+            lo[at] = (half_t)((x - (float)h) * kLoScale);
+        } else if (there) {
+            const int64_t to = transposed ? (int64_t)(j0 + lane) * ld_out + i0 + r : (int64_t)(i0 + r) * ld_out + j0 + lane;
+            out[mat * each_out + to] = __builtin_bit_cast(uint16_t, (__bf16)x);
+        }
+    }
+}
+
+constexpr int64_t kNsMaxSide = 65536;
+
+struct NsLayout {
+    int m, n, mp, np;
+    bool split;
+    size_t parts, scales, diag_a, diag_b, off_a, off_b, off_a_lo, off_b_lo, hi[2], lo[2], total;
+};
+static NsLayout ns_layout(int64_t count, int64_t rows, int64_t cols) {
+    NsLayout L;
+    L.m = (int)std::min(rows, cols);
+    L.n = (int)std::max(rows, cols);
+    L.mp = (L.m + 63) / 64 * 64;
+    L.np = (L.n + 63) / 64 * 64;
+    L.split = L.m < kSplitBelow;
+    size_t o = 0;
+    auto take = [&](size_t each) {
+        const size_t at = o;
+        o += round_up((size_t)count * each, 256);
+        return at;
+    };
+    L.parts = take(kNsParts * sizeof(double));
+    L.scales = take(sizeof(float2));
+    L.diag_a = take((size_t)L.mp * 4);
+    L.diag_b = take((size_t)L.mp * 4);
+    L.off_a = take((size_t)L.mp * L.mp * 2);
+    L.off_b = take((size_t)L.mp * L.mp * 2);
+    L.off_a_lo = L.off_b_lo = L.off_a;
+    if (L.split) {
+        L.off_a_lo = take((size_t)L.mp * L.mp * 2);
+        L.off_b_lo = take((size_t)L.mp * L.mp * 2);
+    }
+    for (int i = 0; i < 2; ++i) {
+        L.hi[i] = take((size_t)L.mp * L.np * 2);
+        L.lo[i] = take((size_t)L.mp * L.np * 2);
+    }
+    L.total = o;
+    return L;
+}
+
+template <class C, NsMode MODE>
+static int launch_ns(NsArgs& p, int64_t count, hipStream_t s) {
+    if (C::kLdsBytes > 64 * 1024 && !allow_lds(reinterpret_cast<const void*>(ns_product_kernel<C, MODE>), C::kLdsBytes)) return TPPO_ERR_LAUNCH;
+    p.tiles_t = (p.n_t + C::kTileT - 1) / C::kTileT;
+    p.tiles_v = (p.n_v + C::kTileV - 1) / C::kTileV;
+    p.tiles = MODE == kGram || MODE == kPoly ? p.tiles_t * (p.tiles_t + 1) / 2 : p.tiles_t * p.tiles_v;
+    hipLaunchKernelGGL((ns_product_kernel<C, MODE>), dim3((unsigned)(p.tiles * count)), dim3(C::kThreads), C::kLdsBytes, s, p);
+    return launch_result();
+}
+
+template <class T>
+static int run_ns(const T* g, int64_t count, int64_t rows, int64_t cols, int64_t ld_g, int64_t stride_g, int steps, float a, float b,
+                  float c, float eps, float scale, uint16_t* out, int64_t ld_out, int64_t stride_out, char* ws, hipStream_t s) {
+    const NsLayout L = ns_layout(count, rows, cols);
+    const bool transposed = rows > cols;
+    double* parts = reinterpret_cast<double*>(ws + L.parts);
+    float2* scales = reinterpret_cast<float2*>(ws + L.scales);
+    const int n_parts = (int)std::min<int64_t>(rows, kNsParts);
+    hipLaunchKernelGGL(ns_norm_kernel<T>, dim3(n_parts, (unsigned)count), dim3(kNsThreads), 0, s, g, (int)rows, (int)cols, ld_g, stride_g, parts);
+    int log2n = 0;
+    while ((2LL << log2n) <= L.n) ++log2n;
+    const float s_scale = (float)(1 << (log2n + 1) / 2);
+    half_t *hi[2], *lo[2];
+    for (int i = 0; i < 2; ++i) {
+        hi[i] = reinterpret_cast<half_t*>(ws + L.hi[i]);
+        lo[i] = reinterpret_cast<half_t*>(ws + L.lo[i]);
+    }
+    hipLaunchKernelGGL(ns_begin_kernel<T>, dim3(L.np / 64, L.mp / 64, (unsigned)count), dim3(kNsThreads), 0, s, g, ld_g, stride_g, parts, n_parts,
+                       eps, scale, s_scale, pow(std::max(1.0, fabs((double)a)), steps), steps ? hi[0] : nullptr, lo[0], scales, L.mp, L.np, L.m,
+                       L.n, transposed, out, ld_out, stride_out);
+    if (hipGetLastError() != hipSuccess) return TPPO_ERR_LAUNCH;
+    NsArgs x = {};
+    x.each_off = (int64_t)L.mp * L.mp;
+    x.each_diag = L.mp;
+    x.each_x = (int64_t)L.mp * L.np;
+    x.ld_off = L.mp;
+    x.ld_x = L.np;
+    x.a = a; x.b = b; x.c = c;
+    x.m = L.m; x.n = L.n; x.transposed = transposed;
+    x.out = out; x.ld_out = ld_out; x.each_out = stride_out; x.scales = scales;
+    half_t *off_a = reinterpret_cast<half_t*>(ws + L.off_a), *off_b = reinterpret_cast<half_t*>(ws + L.off_b);
+    float *diag_a = reinterpret_cast<float*>(ws + L.diag_a), *diag_b = reinterpret_cast<float*>(ws + L.diag_b);
+    half_t *off_a_lo = reinterpret_cast<half_t*>(ws + L.off_a_lo), *off_b_lo = reinterpret_cast<half_t*>(ws + L.off_b_lo);
+    auto bytes = [](const half_t* from, const half_t* to) { return reinterpret_cast<const char*>(to) - reinterpret_cast<const char*>(from); };
+    auto products = [&](auto split) {
+        constexpr bool kSplit = decltype(split)::value;
+        typedef NsCfg<128, 128, 2, 2, false, kSplit> Square;
+        typedef NsCfg<128, 128, 2, 2, true, kSplit> Across;
+        for (int i = 0; i < steps; ++i) {
+            half_t *x_hi = hi[i & 1], *x_lo = lo[i & 1];
+            NsArgs p = x;                            // A = X X^T
+            p.t_op = p.v_op = x_hi;
+            p.lo_t = p.lo_v = bytes(x_hi, x_lo);
+            p.ld_t = p.ld_v = L.np;
+            p.each_t = p.each_v = x.each_x;
+            p.n_t = p.n_v = L.mp;
+            p.k = L.np;
+            p.off = off_a; p.off_lo = off_a_lo; p.diag = diag_a;
+            if (const int rc = launch_ns<Square, kGram>(p, count, s)) return rc;
+            p = x;                                   // B = b A + c A A
+            p.t_op = p.v_op = off_a;
+            p.lo_t = p.lo_v = bytes(off_a, off_a_lo);
+            p.ld_t = p.ld_v = L.mp;
+            p.each_t = p.each_v = x.each_off;
+            p.n_t = p.n_v = p.k = L.mp;
+            p.off = off_a; p.off_lo = off_a_lo; p.diag = diag_a;
+            p.off_out = off_b; p.off_out_lo = off_b_lo; p.diag_out = diag_b;
+            if (const int rc = launch_ns<Square, kPoly>(p, count, s)) return rc;
+            p = x;                                   // X = a X + B X
+            p.t_op = off_b; p.lo_t = bytes(off_b, off_b_lo); p.ld_t = L.mp; p.each_t = x.each_off; p.n_t = L.mp;
+            p.v_op = x_hi; p.lo_v = bytes(x_hi, x_lo); p.ld_v = L.np; p.each_v = x.each_x; p.n_v = L.np;
+            p.k = L.mp;
+            p.diag = diag_b; p.hi = x_hi; p.lo = x_lo; p.hi_out = hi[~i & 1]; p.lo_out = lo[~i & 1];
+            if (const int rc = i + 1 < steps ? launch_ns<Across, kUpdate>(p, count, s) : launch_ns<Across, kLast>(p, count, s)) return rc;
+        }
+        return (int)TPPO_OK;
+    };
+    return L.split ? products(std::true_type()) : products(std::false_type());
+}
+
+}  // namespace tppo
+
+extern "C" size_t tppo_orthogonalize_workspace_bytes(int64_t count, int64_t rows, int64_t cols) {
+    using namespace tppo;
+    if (count < 1 || rows < 1 || cols < 1 || rows > kNsMaxSide || cols > kNsMaxSide || count > INT32_MAX / 2) return 256;
+    return ns_layout(count, rows, cols).total;
+}
+
+extern "C" int tppo_orthogonalize(const void* g, int64_t count, int64_t rows, int64_t cols, int64_t ld_g, int64_t stride_g, tppo_dtype dt,
+                                  int32_t steps, float a, float b, float c, float eps, float scale, void* out, int64_t ld_out,
+                                  int64_t stride_out, void* workspace, size_t workspace_bytes, void* stream) {
+    using namespace tppo;
+    if (dt != TPPO_F32 && dt != TPPO_BF16) return TPPO_ERR_DTYPE;
+    if (count < 0 || count > 65535 || rows < 1 || cols < 1 || rows > kNsMaxSide || cols > kNsMaxSide || ld_g < cols || ld_out < cols)
+        return TPPO_ERR_SIZE;
+    if (count > 1 && (stride_g < 0 || stride_out < (rows - 1) * ld_out + cols)) return TPPO_ERR_SIZE;
+    if (steps < 0 || steps > 64 || !(eps >= 0.f)) return TPPO_ERR_PARAM;
+    for (float v : {a, b, c, eps, scale})
+        if (!(v - v == 0.f)) return TPPO_ERR_PARAM;
+    if (count == 0) return TPPO_OK;
+    if (!g || !out) return TPPO_ERR_NULL;
+    if (!is_aligned(g, dt == TPPO_F32 ? 4 : 2) || !is_aligned(out, 2)) return TPPO_ERR_PARAM;
+    const NsLayout L = ns_layout(count, rows, cols);
+    // (tiles of the whole stack are numbered in 32 bits)
+    if (count * ((L.mp / 64) * (int64_t)(L.np / 64)) > INT32_MAX) return TPPO_ERR_SIZE;
+    if (!workspace || !is_aligned(workspace, 256) || workspace_bytes < L.total) return TPPO_ERR_WORKSPACE;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    if (dt == TPPO_F32)
+        return run_ns(static_cast<const float*>(g), count, rows, cols, ld_g, stride_g, steps, a, b, c, eps, scale, static_cast<uint16_t*>(out),
+                      ld_out, stride_out, static_cast<char*>(workspace), s);
+    return run_ns(static_cast<const uint16_t*>(g), count, rows, cols, ld_g, stride_g, steps, a, b, c, eps, scale, static_cast<uint16_t*>(out),
+                  ld_out, stride_out, static_cast<char*>(workspace), s);
+}

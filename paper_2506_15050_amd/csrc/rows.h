@@ -1,0 +1,104 @@
+// Rows of fp32 or bf16 in 16-byte pieces, for the kernels that take whole rows at any stride and address (layer norm, balance loss).
+#pragma once
+#include <type_traits>
+
+#include "common.h"
+
+namespace tppo {
+
+// A piece of a row: 16 bytes, from any address that the type allows (the hardware takes vector accesses at any, across lines more slowly).
+template <class T>
+struct Piece;
+template <>
+struct Piece<float> {
+    static constexpr int kN = 4;
+    typedef float V __attribute__((ext_vector_type(4), aligned(4)));
+    V v;
+    __device__ __forceinline__ float get(int e) const { return v[e]; }
+    __device__ __forceinline__ void set(int e, float x) { v[e] = x; }
+};
+template <>
+struct Piece<uint16_t> {                             // bf16
+    static constexpr int kN = 8;
+    typedef uint32_t V __attribute__((ext_vector_type(4), aligned(2)));
+    V v;
+    __device__ __forceinline__ float get(int e) const {
+        return __uint_as_float(e & 1 ? v[e >> 1] & 0xFFFF0000u : v[e >> 1] << 16);
+    }
+};
+
+__device__ __forceinline__ float to_f32(float x) { return x; }
+__device__ __forceinline__ float to_f32(uint16_t x) { return __uint_as_float((uint32_t)x << 16); }
+
+// two fp32 -> two bf16 in one instruction, round to nearest even
+__device__ __forceinline__ uint32_t two_bf16(float lo, float hi) {
+    typedef float f2 __attribute__((ext_vector_type(2)));
+    typedef __bf16 b2 __attribute__((ext_vector_type(2)));
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector((f2{lo, hi}), b2));
+}
+__device__ __forceinline__ void put(float* p, float x) { *p = x; }
+__device__ __forceinline__ void put(uint16_t* p, float x) { *p = (uint16_t)two_bf16(x, 0.f); }
+
+// Elements c * kN .. of a row of n; what lies beyond the row is `beyond` and not read.  RAGGED: n is no multiple of kN.
+template <class T, bool RAGGED>
+__device__ __forceinline__ Piece<T> piece_at(const T* row, int c, int n, float beyond = 0.f) {
+    constexpr int kN = Piece<T>::kN;
+    Piece<T> p;
+    if (!RAGGED || (c + 1) * kN <= n) {
+        p.v = *reinterpret_cast<const typename Piece<T>::V*>(row + c * kN);
+    } else {
+        if constexpr (kN == 4) {
+#pragma unroll
+            for (int e = 0; e < kN; ++e) p.v[e] = c * kN + e < n ? row[c * kN + e] : beyond;
+        } else {
+            const uint32_t b = two_bf16(beyond, beyond);
+#pragma unroll
+            for (int e = 0; e < kN; e += 2) {
+                const uint32_t lo = c * kN + e < n ? row[c * kN + e] : b & 0xFFFFu;
+                const uint32_t hi = c * kN + e + 1 < n ? row[c * kN + e + 1] : b & 0xFFFFu;
+                p.v[e >> 1] = lo | hi << 16;
+            }
+        }
+    }
+    return p;
+}
+
+// kIn values to elements c * kIn .. of a row of n of type T
+template <class T, int kIn, bool RAGGED>
+__device__ __forceinline__ void put_piece(T* row, int c, int n, const float (&x)[kIn]) {
+    T* at = row + c * kIn;
+    if (!RAGGED || (c + 1) * kIn <= n) {
+        if constexpr (sizeof(T) == 4) {
+#pragma unroll
+            for (int e = 0; e < kIn; e += 4)
+                *reinterpret_cast<Piece<float>::V*>(at + e) = Piece<float>::V{x[e], x[e + 1], x[e + 2], x[e + 3]};
+        } else {
+            static_assert(kIn == 8, "16 bytes");
+            *reinterpret_cast<Piece<uint16_t>::V*>(at) = Piece<uint16_t>::V{two_bf16(x[0], x[1]), two_bf16(x[2], x[3]),
+                                                                            two_bf16(x[4], x[5]), two_bf16(x[6], x[7])};
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < kIn; ++e)
+            if (c * kIn + e < n) put(at + e, x[e]);
+    }
+}
+
+// kOut values of type T from elements c * kOut .. of a row of n
+template <class T, int kOut, bool RAGGED>
+__device__ __forceinline__ void get_piece(const T* row, int c, int n, float (&x)[kOut]) {
+    constexpr int kN = Piece<T>::kN;
+#pragma unroll
+    for (int q = 0; q < kOut / kN; ++q) {
+        const Piece<T> p = piece_at<T, RAGGED>(row, c * (kOut / kN) + q, n);
+#pragma unroll
+        for (int e = 0; e < kN; ++e) x[q * kN + e] = p.get(e);
+    }
+}
+
+// the wavefront's sum, in every lane
+__device__ __forceinline__ float wave_sum(float x) {
+    return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(wave_prefix(x)), kWave - 1));
+}
+
+}  // namespace tppo

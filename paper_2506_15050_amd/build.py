@@ -15,7 +15,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libtppo.so")
 MARSHAL = os.path.join(HERE, "_marshal.so")
 SOURCES = ["plan.hip", "select.hip", "egae.hip", "losses.hip", "head.hip", "head_bwd.hip", "value_head.hip", "diag.hip",
-           "layer_norm.hip", "balance.hip", "ortho.hip", "batcher.cpp"]
+           "layer_norm.hip", "balance.hip", "ortho.hip", "ortho_gram.hip", "batcher.cpp"]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
          "-Wall", "-Wno-unused-function", "-Wno-inline-asm"]

@@ -13,16 +13,11 @@
 // one pass  m = 512 rank one 1.5e-3, full 7e-4;  256 2.3e-3;  64 9e-3;  three passes  1e-4 at most.
 // All scales are powers of two: X is held times S = 2^round(log2(n) / 2), so that entries are around one from the first step to the last,
 // A and B off the diagonal times 64.  Where |G|_F is so far below eps that X stays under 1/4 to the end, S is larger by as much.
-#include "head_tile.h"
+#include "ortho.h"
 
 namespace tppo {
 
-typedef _Float16 half_t;
-typedef half_t half8 __attribute__((ext_vector_type(8)));
-typedef half_t half4 __attribute__((ext_vector_type(4)));
-
-constexpr float kLoScale = 2048.f, kOffScale = 64.f;
-constexpr int kSplitBelow = 512;
+constexpr int kSplitBelow = kGramBelow;
 
 enum NsMode { kGram, kPoly, kUpdate, kLast };        // A = X X^T;  B = b A + c A A;  X = a X + B X;  the same into the caller's array
 
@@ -56,11 +51,7 @@ struct NsCfg {
     static constexpr bool kKMajor = KMAJOR, kSplit = SPLIT;
     static constexpr int kKRowBytes = TV * 2;        // K-major: a stage is 64 rows of TV columns
     static_assert(kDmaPerWave * kWaves == kDma && kDma * 1024 == kStageBytes, "whole transfers");
-    static_assert(!KMAJOR || TV % 128 == 0, "the swizzle of K-major rows spans 256 bytes");
 };
-
-__device__ __forceinline__ int ns_swz(int r) { return (r >> 1) & 7; }
-__device__ __forceinline__ int ns_swz_k(int k) { return ((k & 3) | ((k >> 3) & 1) << 2) << 1; }
 
 // Tile `id` of a matrix.  Rectangular: blocks of 8 T tiles, column by column, so that an XCD's workgroups share operands in its L2.
 // Symmetric: the same over v >= t.
@@ -100,8 +91,7 @@ __global__ __launch_bounds__(C::kThreads, C::kLdsBytes <= 80 * 1024 ? C::kWaves 
     constexpr bool kSymmetric = MODE == kGram || MODE == kPoly;
     constexpr int kVB = C::kVB, kTB = C::kTB, kDmaPerWave = C::kDmaPerWave;
     extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
-    // workgroups go round-robin over the 8 XCDs: consecutive tiles to each (one more to the first gridDim.x % 8 of them)
-    const int xcd = (int)blockIdx.x & 7, id = xcd * ((int)gridDim.x >> 3) + min(xcd, (int)gridDim.x & 7) + ((int)blockIdx.x >> 3);
+    const int id = ns_by_xcd(blockIdx.x, gridDim.x);
     const int mat = id / p.tiles;
     int tile_t, tile_v;
     ns_tile_at<kSymmetric>(id - mat * p.tiles, p.tiles_t, p.tiles_v, tile_t, tile_v);
@@ -118,7 +108,7 @@ __global__ __launch_bounds__(C::kThreads, C::kLdsBytes <= 80 * 1024 ? C::kWaves 
         const int d = wave * kDmaPerWave + q;
         if (d < C::kDmaV && C::kKMajor) {
             constexpr int kPerRow = C::kKRowBytes / 16;
-            const int at = d * 64 + lane, k = at / kPerRow, c = (at % kPerRow) ^ ns_swz_k(k);
+            const int at = d * 64 + lane, k = at / kPerRow, c = (at % kPerRow) ^ ns_swz_k<C::kTileV>(k);
             src[q] = v_base + ((int64_t)k * p.ld_v + min(v0 + c * 8, p.n_v - 8)) * 2;
         } else {
             const int r = (d < C::kDmaV ? d : d - C::kDmaV) * 8 + (lane >> 3), staged = d * 8 + (lane >> 3);
@@ -161,14 +151,7 @@ __global__ __launch_bounds__(C::kThreads, C::kLdsBytes <= 80 * 1024 ? C::kWaves 
         const int k32 = step / kVB, vb = step % kVB, c = k32 * 4 + grp;
         const unsigned char* st = smem + stage * C::kStageBytes;
         if constexpr (C::kKMajor) {
-            typedef short s4 __attribute__((ext_vector_type(4)));
-            typedef __attribute__((address_space(3))) s4* lds_s4;
-            const int k = grp * 8 + (col >> 2), first = wv * kVB + vb;
-            const int lane_at = k * C::kKRowBytes + ((2 * first + ((col & 3) >> 1)) ^ ns_swz_k(k)) * 16 + (col & 1) * 8;
-            const unsigned from = lds_base + stage * C::kStageBytes + lane_at + k32 * 32 * C::kKRowBytes;
-            const s4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4)(size_t)from);
-            const s4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4)(size_t)(from + 4 * C::kKRowBytes));
-            fa[step & 1] = __builtin_bit_cast(half8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+            fa[step & 1] = ns_k_major_frag<C::kTileV>(lds_base + stage * C::kStageBytes, wv * kVB + vb, k32, lane);
         } else {
             const int r = wv * C::kWaveV + vb * 16 + col;
             fa[step & 1] = *reinterpret_cast<const half8*>(st + r * C::kRowBytes + ((c ^ ns_swz(r)) << 4));
@@ -302,7 +285,7 @@ __global__ __launch_bounds__(C::kThreads, C::kLdsBytes <= 80 * 1024 ? C::kWaves 
                         new_lo[e] = (half_t)((x - (float)new_hi[e]) * kLoScale);
                     } else if (t < p.m && v + e < p.n) {
                         const int64_t to = p.transposed ? (int64_t)(v + e) * p.ld_out + t : (int64_t)t * p.ld_out + v + e;
-                        p.out[mat * p.each_out + to] = (uint16_t)__builtin_bit_cast(uint16_t, (__bf16)(x * scales.y));
+                        p.out[mat * p.each_out + to] = ns_bf16(x * scales.y);
                     }
                 }
                 if constexpr (MODE == kUpdate) {
@@ -385,7 +368,7 @@ __global__ __launch_bounds__(kNsThreads) void ns_begin_kernel(const T* g, int64_
             lo[at] = (half_t)((x - (float)h) * kLoScale);
         } else if (there) {
             const int64_t to = transposed ? (int64_t)(j0 + lane) * ld_out + i0 + r : (int64_t)(i0 + r) * ld_out + j0 + lane;
-            out[mat * each_out + to] = __builtin_bit_cast(uint16_t, (__bf16)x);
+            out[mat * each_out + to] = ns_bf16(x);
         }
     }
 }
@@ -395,7 +378,7 @@ constexpr int64_t kNsMaxSide = 65536;
 struct NsLayout {
     int m, n, mp, np;
     bool split;
-    size_t parts, scales, diag_a, diag_b, off_a, off_b, off_a_lo, off_b_lo, hi[2], lo[2], total;
+    size_t parts, scales, shared, diag_a, diag_b, off_a, off_b, off_a_lo, off_b_lo, hi[2], lo[2], total;
 };
 static NsLayout ns_layout(int64_t count, int64_t rows, int64_t cols) {
     NsLayout L;
@@ -412,6 +395,9 @@ static NsLayout ns_layout(int64_t count, int64_t rows, int64_t cols) {
     };
     L.parts = take(kNsParts * sizeof(double));
     L.scales = take(sizeof(float2));
+    L.hi[0] = take((size_t)L.mp * L.np * 2);
+    L.lo[0] = take((size_t)L.mp * L.np * 2);
+    L.shared = o;                                    // what the two ways need from here on
     L.diag_a = take((size_t)L.mp * 4);
     L.diag_b = take((size_t)L.mp * 4);
     L.off_a = take((size_t)L.mp * L.mp * 2);
@@ -421,10 +407,9 @@ static NsLayout ns_layout(int64_t count, int64_t rows, int64_t cols) {
         L.off_a_lo = take((size_t)L.mp * L.mp * 2);
         L.off_b_lo = take((size_t)L.mp * L.mp * 2);
     }
-    for (int i = 0; i < 2; ++i) {
-        L.hi[i] = take((size_t)L.mp * L.np * 2);
-        L.lo[i] = take((size_t)L.mp * L.np * 2);
-    }
+    L.hi[1] = take((size_t)L.mp * L.np * 2);
+    L.lo[1] = take((size_t)L.mp * L.np * 2);
+    if (L.m < kGramBelow) o = std::max(o, L.shared + ns_gram_bytes(count, L.m, L.n));
     L.total = o;
     return L;
 }
@@ -437,6 +422,30 @@ static int launch_ns(NsArgs& p, int64_t count, hipStream_t s) {
     p.tiles = MODE == kGram || MODE == kPoly ? p.tiles_t * (p.tiles_t + 1) / 2 : p.tiles_t * p.tiles_v;
     hipLaunchKernelGGL((ns_product_kernel<C, MODE>), dim3((unsigned)(p.tiles * count)), dim3(C::kThreads), C::kLdsBytes, s, p);
     return launch_result();
+}
+
+// Side of the output tiles.  256 x 256 tiles read the least, a workgroup to a CU; 128 x 128 ones, two to a CU, spread fewer of them and leave
+// less of a last round empty.  Times in us: a stage (64 of the contraction) of a large tile 1.4, of two small ones that share a CU 1.1, of
+// one that has it alone 0.77; and what a round's tiles do to memory when they end.  Measured, a call, 128 -> 256:  5120 x 5120: 3560 -> 2910;
+// 4096: 2330 -> 2040;  where the rule says 128: 3584: 1479 (1591; its products B X, which go by themselves, 139 -> 109);  2048: 548 (991);
+// 1024 x 4096: 544 (974);  twelve of 1024 x 1024: 617 (689).  (192 x 192, whose tiles fill the rounds of 4096 and 5120 best, asks as much of
+// L2 as 128 x 128 does: 1990 and 3420.)
+static int ns_tile_side(const NsArgs& p, int64_t count, bool symmetric, int stages) {
+    auto tiles = [&](int side) {
+        const int64_t t = (p.n_t + side - 1) / side, v = (p.n_v + side - 1) / side;
+        return (symmetric ? t * (t + 1) / 2 : t * v) * count;
+    };
+    const double end = symmetric ? 8.0 : 25.0;
+    const int64_t each = (tiles(128) + kSweepGroups - 1) / kSweepGroups;       // small tiles on the busiest CU
+    const double small = (double)(each / 2) * (1.1 * stages + end / 2) + (double)(each % 2) * (0.77 * stages + end / 4);
+    return rounds_of(tiles(256)) * (1.4 * stages + end) < small ? 256 : 128;
+}
+template <bool SPLIT, NsMode MODE>
+static int launch_ns_tiles(NsArgs& p, int64_t count, hipStream_t s) {
+    constexpr bool kAcross = MODE == kUpdate || MODE == kLast;
+    const int side = ns_tile_side(p, count, !kAcross, p.k / 64 * (SPLIT ? 3 : 1));
+    if (side == 256) return launch_ns<NsCfg<256, 256, 2, 4, kAcross, SPLIT>, MODE>(p, count, s);
+    return launch_ns<NsCfg<128, 128, 2, 2, kAcross, SPLIT>, MODE>(p, count, s);
 }
 
 template <class T>
@@ -469,14 +478,16 @@ static int run_ns(const T* g, int64_t count, int64_t rows, int64_t cols, int64_t
     x.a = a; x.b = b; x.c = c;
     x.m = L.m; x.n = L.n; x.transposed = transposed;
     x.out = out; x.ld_out = ld_out; x.each_out = stride_out; x.scales = scales;
+    if (L.m < kGramBelow && ns_gram_fits(steps, a, b, c)) {
+        const NsShape shape = {L.m, L.n, L.mp, L.np, transposed, count, steps, a, b, c, out, ld_out, stride_out};
+        return ns_gram(shape, hi[0], lo[0], scales, ws + L.shared, s);
+    }
     half_t *off_a = reinterpret_cast<half_t*>(ws + L.off_a), *off_b = reinterpret_cast<half_t*>(ws + L.off_b);
     float *diag_a = reinterpret_cast<float*>(ws + L.diag_a), *diag_b = reinterpret_cast<float*>(ws + L.diag_b);
     half_t *off_a_lo = reinterpret_cast<half_t*>(ws + L.off_a_lo), *off_b_lo = reinterpret_cast<half_t*>(ws + L.off_b_lo);
     auto bytes = [](const half_t* from, const half_t* to) { return reinterpret_cast<const char*>(to) - reinterpret_cast<const char*>(from); };
     auto products = [&](auto split) {
         constexpr bool kSplit = decltype(split)::value;
-        typedef NsCfg<128, 128, 2, 2, false, kSplit> Square;
-        typedef NsCfg<128, 128, 2, 2, true, kSplit> Across;
         for (int i = 0; i < steps; ++i) {
             half_t *x_hi = hi[i & 1], *x_lo = lo[i & 1];
             NsArgs p = x;                            // A = X X^T
@@ -487,7 +498,7 @@ static int run_ns(const T* g, int64_t count, int64_t rows, int64_t cols, int64_t
             p.n_t = p.n_v = L.mp;
             p.k = L.np;
             p.off = off_a; p.off_lo = off_a_lo; p.diag = diag_a;
-            if (const int rc = launch_ns<Square, kGram>(p, count, s)) return rc;
+            if (const int rc = launch_ns_tiles<kSplit, kGram>(p, count, s)) return rc;
             p = x;                                   // B = b A + c A A
             p.t_op = p.v_op = off_a;
             p.lo_t = p.lo_v = bytes(off_a, off_a_lo);
@@ -496,13 +507,13 @@ static int run_ns(const T* g, int64_t count, int64_t rows, int64_t cols, int64_t
             p.n_t = p.n_v = p.k = L.mp;
             p.off = off_a; p.off_lo = off_a_lo; p.diag = diag_a;
             p.off_out = off_b; p.off_out_lo = off_b_lo; p.diag_out = diag_b;
-            if (const int rc = launch_ns<Square, kPoly>(p, count, s)) return rc;
+            if (const int rc = launch_ns_tiles<kSplit, kPoly>(p, count, s)) return rc;
             p = x;                                   // X = a X + B X
             p.t_op = off_b; p.lo_t = bytes(off_b, off_b_lo); p.ld_t = L.mp; p.each_t = x.each_off; p.n_t = L.mp;
             p.v_op = x_hi; p.lo_v = bytes(x_hi, x_lo); p.ld_v = L.np; p.each_v = x.each_x; p.n_v = L.np;
             p.k = L.mp;
             p.diag = diag_b; p.hi = x_hi; p.lo = x_lo; p.hi_out = hi[~i & 1]; p.lo_out = lo[~i & 1];
-            if (const int rc = i + 1 < steps ? launch_ns<Across, kUpdate>(p, count, s) : launch_ns<Across, kLast>(p, count, s)) return rc;
+            if (const int rc = i + 1 < steps ? launch_ns_tiles<kSplit, kUpdate>(p, count, s) : launch_ns_tiles<kSplit, kLast>(p, count, s)) return rc;
         }
         return (int)TPPO_OK;
     };

@@ -14,6 +14,7 @@
 // All scales are powers of two: X is held times S = 2^round(log2(n) / 2), so that entries are around one from the first step to the last,
 // A and B off the diagonal times 64.  Where |G|_F is so far below eps that X stays under 1/4 to the end, S is larger by as much.
 #include "ortho.h"
+#include "rows.h"
 
 namespace tppo {
 
@@ -298,12 +299,7 @@ __global__ __launch_bounds__(C::kThreads, C::kLdsBytes <= 80 * 1024 ? C::kWaves 
 }
 
 // ---- |G|_F and the first X
-constexpr int kNsThreads = 256, kNsParts = 64;       // partial sums of squares a matrix
-template <class T>
-__device__ __forceinline__ float ns_value(const T* p) {
-    if constexpr (sizeof(T) == 4) return *p;
-    else return __uint_as_float((uint32_t)*p << 16);
-}
+constexpr int kNsThreads = 256, kNsParts = 512;      // partial sums of squares a matrix
 __device__ __forceinline__ double ns_workgroup_sum(double x, double* place) {
     x = wave_prefix(x);
     if ((threadIdx.x & 63) == 63) place[threadIdx.x >> 6] = x;
@@ -313,62 +309,90 @@ __device__ __forceinline__ double ns_workgroup_sum(double x, double* place) {
     for (int w = 0; w < kNsThreads / kWave; ++w) x += place[w];
     return x;
 }
-// (in 64 bits: squares of large fp32 values overflow, and nothing here is bound by arithmetic)
-template <class T>
-__global__ __launch_bounds__(kNsThreads) void ns_norm_kernel(const T* g, int rows, int cols, int64_t ld, int64_t each, double* parts) {
+// Bound by memory: 16 bytes a thread, wherever rows begin.  (In 64 bits: squares of large fp32 values overflow.)
+template <class T, bool RAGGED>
+__global__ __launch_bounds__(kNsThreads) void ns_norm_kernel(const T* __restrict__ g, int rows, int cols, int64_t ld, int64_t each,
+                                                             double* __restrict__ parts) {
+    constexpr int kN = Piece<T>::kN;
     __shared__ double place[kNsThreads / kWave];
     const T* from = g + blockIdx.y * each;
+    const unsigned per_row = (cols + kN - 1) / kN, all = per_row * rows;                       // (2^30 at most)
     double sum = 0.0;
-    for (int r = blockIdx.x; r < rows; r += gridDim.x)
-        for (int c = threadIdx.x; c < cols; c += kNsThreads) {
-            const double x = (double)ns_value(from + (int64_t)r * ld + c);
-            sum = fma(x, x, sum);
-        }
+#pragma unroll 4
+    for (unsigned i = blockIdx.x * kNsThreads + threadIdx.x; i < all; i += gridDim.x * kNsThreads) {
+        const unsigned r = i / per_row, c = i - r * per_row;
+        const Piece<T> p = piece_at<T, RAGGED>(from + (int64_t)r * ld, c, cols);
+#pragma unroll
+        for (int e = 0; e < kN; ++e) sum = fma((double)p.get(e), (double)p.get(e), sum);
+    }
     sum = ns_workgroup_sum(sum, place);
     if (threadIdx.x == 0) parts[(int64_t)blockIdx.y * kNsParts + blockIdx.x] = sum;
 }
 
-// X [mp, np], zeros beyond m x n, from G or its transpose, in tiles of 64 x 64 through LDS.  hi == NULL: no products follow, X times
-// out_scale goes to the caller's array.
+// X [mp, np], zeros beyond m x n, from G or its transpose (through LDS), a 64 x 64 tile a workgroup's turn.  hi == NULL: no products follow, X
+// times `scale` goes to the caller's array.
 template <class T>
-__global__ __launch_bounds__(kNsThreads) void ns_begin_kernel(const T* g, int64_t ld, int64_t each, const double* parts, int count_parts,
-                                                              float eps, float scale, float s_scale, double growth, half_t* hi, half_t* lo,
-                                                              float2* scales, int mp, int np, int m, int n, int transposed,
-                                                              uint16_t* out, int64_t ld_out, int64_t each_out) {
+__global__ __launch_bounds__(kNsThreads) void ns_begin_kernel(const T* __restrict__ g, int64_t ld, int64_t each, const double* __restrict__ parts,
+                                                              int count_parts, float eps, float scale, float s_scale, double growth,
+                                                              half_t* __restrict__ hi, half_t* __restrict__ lo, float2* scales, int mp, int np,
+                                                              int m, int n, int transposed, uint16_t* __restrict__ out, int64_t ld_out,
+                                                              int64_t each_out) {
     __shared__ double place[kNsThreads / kWave];
     __shared__ float tile[64][65];
-    const int mat = blockIdx.z;
+    const int mat = blockIdx.y;
     double sum = 0.0;
-    if ((int)threadIdx.x < count_parts) sum = parts[(int64_t)mat * kNsParts + threadIdx.x];
+    for (int i = threadIdx.x; i < count_parts; i += kNsThreads) sum += parts[(int64_t)mat * kNsParts + i];
     sum = ns_workgroup_sum(sum, place);
     const double norm = sqrt(sum) + (double)eps;
-    // (one of zeros with eps = 0 gives NaN, as 0 / 0 does; an infinity in G makes all of it NaN)
     // growth: what the steps make of small singular values
     const double most = sqrt(sum) / norm * growth;
     const double lift = hi && most > 0.0 && most < 0.25 ? ldexp(1.0, -ilogb(most) - 3) : 1.0;
     const double s_all = hi ? (double)s_scale * lift : (double)scale;
+    // (one of zeros with eps = 0 gives NaN, as 0 / 0 does; an infinity in G makes all of it NaN)
     const double by = norm < 1.0e300 ? s_all / norm : __builtin_nan("");
-    if (hi && threadIdx.x == 0 && blockIdx.x == 0 && blockIdx.y == 0)
-        scales[mat] = make_float2((float)(1.0 / (s_all * s_all)), (float)((double)scale / s_all));
+    if (hi && threadIdx.x == 0 && blockIdx.x == 0) scales[mat] = make_float2((float)(1.0 / (s_all * s_all)), (float)((double)scale / s_all));
     const T* from = g + mat * each;
-    const int i0 = blockIdx.y * 64, j0 = blockIdx.x * 64, lane = threadIdx.x & 63, part = threadIdx.x >> 6;
-    if (transposed) {                                // G is [n, m]
-        for (int r = part; r < 64; r += 4) tile[lane][r] = j0 + r < n && i0 + lane < m ? ns_value(from + (int64_t)(j0 + r) * ld + i0 + lane) : 0.f;
-    } else {
-        for (int r = part; r < 64; r += 4) tile[r][lane] = i0 + r < m && j0 + lane < n ? ns_value(from + (int64_t)(i0 + r) * ld + j0 + lane) : 0.f;
-    }
-    __syncthreads();
-    for (int r = part; r < 64; r += 4) {
-        const bool there = i0 + r < m && j0 + lane < n;
-        const float x = there ? (float)((double)tile[r][lane] * by) : 0.f;
-        if (hi) {
-            const int64_t at = ((int64_t)mat * mp + i0 + r) * np + j0 + lane;
-            const half_t h = (half_t)x;
-            hi[at] = h;
-            lo[at] = (half_t)((x - (float)h) * kLoScale);
-        } else if (there) {
-            const int64_t to = transposed ? (int64_t)(j0 + lane) * ld_out + i0 + r : (int64_t)(i0 + r) * ld_out + j0 + lane;
-            out[mat * each_out + to] = ns_bf16(x);
+    const int tiles_n = np / 64, tiles = tiles_n * (mp / 64);
+    for (int id = blockIdx.x; id < tiles; id += gridDim.x) {
+        const int i0 = id / tiles_n * 64, j0 = (id - id / tiles_n * tiles_n) * 64;
+        if (transposed) {                            // G is [n, m]
+            const int lane = threadIdx.x & 63;
+            __syncthreads();
+#pragma unroll 4
+            for (int r = threadIdx.x >> 6; r < 64; r += 4)
+                tile[lane][r] = j0 + r < n && i0 + lane < m ? to_f32(from[(int64_t)(j0 + r) * ld + i0 + lane]) : 0.f;
+            __syncthreads();
+        }
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {       // eight columns of a row
+            const int r = half * 32 + (threadIdx.x >> 3), c = (threadIdx.x & 7) * 8, i = i0 + r, j = j0 + c;
+            float x[8];
+            if (transposed) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) x[e] = tile[r][c + e];
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) x[e] = 0.f;
+                if (i < m && j < n) get_piece<T, 8, true>(from + (int64_t)i * ld, j / 8, n, x);
+            }
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] = (float)((double)x[e] * by);
+            if (hi) {
+                half8 h, l;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const float y = i < m && j + e < n ? x[e] : 0.f;                           // (zeros, also where `by` is no number)
+                    h[e] = (half_t)y;
+                    l[e] = (half_t)((y - (float)h[e]) * kLoScale);
+                }
+                const int64_t at = ((int64_t)mat * mp + i) * np + j;
+                *reinterpret_cast<half8*>(hi + at) = h;
+                *reinterpret_cast<half8*>(lo + at) = l;
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    if (i < m && j + e < n) out[mat * each_out + (transposed ? (int64_t)(j + e) * ld_out + i : (int64_t)i * ld_out + j + e)] = ns_bf16(x[e]);
+            }
         }
     }
 }
@@ -455,8 +479,12 @@ static int run_ns(const T* g, int64_t count, int64_t rows, int64_t cols, int64_t
     const bool transposed = rows > cols;
     double* parts = reinterpret_cast<double*>(ws + L.parts);
     float2* scales = reinterpret_cast<float2*>(ws + L.scales);
-    const int n_parts = (int)std::min<int64_t>(rows, kNsParts);
-    hipLaunchKernelGGL(ns_norm_kernel<T>, dim3(n_parts, (unsigned)count), dim3(kNsThreads), 0, s, g, (int)rows, (int)cols, ld_g, stride_g, parts);
+    // (a workgroup for every 1024 pieces of 16 bytes, four to a CU over the whole stack, eight a matrix whatever its size)
+    constexpr int kN = Piece<T>::kN;
+    const int64_t pieces = rows * ((cols + kN - 1) / kN);
+    const int n_parts = (int)std::max<int64_t>(1, std::min<int64_t>({(pieces + 1023) / 1024, kNsParts, std::max<int64_t>(1024 / count, 8)}));
+    hipLaunchKernelGGL((cols % kN ? ns_norm_kernel<T, true> : ns_norm_kernel<T, false>), dim3(n_parts, (unsigned)count), dim3(kNsThreads), 0, s, g,
+                       (int)rows, (int)cols, ld_g, stride_g, parts);
     int log2n = 0;
     while ((2LL << log2n) <= L.n) ++log2n;
     const float s_scale = (float)(1 << (log2n + 1) / 2);
@@ -465,7 +493,8 @@ static int run_ns(const T* g, int64_t count, int64_t rows, int64_t cols, int64_t
         hi[i] = reinterpret_cast<half_t*>(ws + L.hi[i]);
         lo[i] = reinterpret_cast<half_t*>(ws + L.lo[i]);
     }
-    hipLaunchKernelGGL(ns_begin_kernel<T>, dim3(L.np / 64, L.mp / 64, (unsigned)count), dim3(kNsThreads), 0, s, g, ld_g, stride_g, parts, n_parts,
+    const int64_t begin_tiles = (int64_t)(L.np / 64) * (L.mp / 64);
+    hipLaunchKernelGGL(ns_begin_kernel<T>, dim3((unsigned)std::min<int64_t>(begin_tiles, 2048), (unsigned)count), dim3(kNsThreads), 0, s, g, ld_g, stride_g, parts, n_parts,
                        eps, scale, s_scale, pow(std::max(1.0, fabs((double)a)), steps), steps ? hi[0] : nullptr, lo[0], scales, L.mp, L.np, L.m,
                        L.n, transposed, out, ld_out, stride_out);
     if (hipGetLastError() != hipSuccess) return TPPO_ERR_LAUNCH;

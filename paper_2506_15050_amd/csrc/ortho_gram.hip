@@ -4,8 +4,9 @@
 // X is read twice instead of twice a step, and what is left between is m x m: 6 m^2 n + 17 m^3 flop (5 steps, halves of symmetric
 // results not counted) against 15 m^2 n + 5 m^3.
 // Precision.  A holds squares of singular values, and its errors where they are small grow by a^2 a step.  So everything here is a pair of
-// fp16, 22 bits, products are hi hi + (hi lo + lo hi) / 2048 with both sums in fp32, and results are taken from one side of the diagonal:
-// emulated against 64 bits 1.3e-3 of the result's norm at worst (2 x 3, singular values 1 and 0.01), 5e-4 from 64 on.
+// fp16, hi + lo, rounded to nearest, 22 bits of what is not far below 1, products are hi hi + hi lo + lo hi with sums in fp32, and A is made
+// symmetric to the bit, step by step.  Emulated against 64 bits: 1.6e-3 of the result's norm at worst (2 x 3, singular values 1 and 0.01), 1e-3
+// from 64 on; with halves cut instead of rounded three times that.  (X itself, whose entries are smaller, has its low halves times 2048.)
 #include "ortho.h"
 
 namespace tppo {
@@ -39,9 +40,33 @@ __device__ __forceinline__ void pair_tile_at(int id, int& t, int& v) {
     t = id - v * (v + 1) / 2;
 }
 
-// 64 x 64 tiles, four wavefronts of 32 x 32.  A stage holds 64 of K of both operands' halves, a quarter of it loaded by each wavefront.
-template <PairMode MODE>
-__global__ __launch_bounds__(kPairThreads, 2) void ns_pair_kernel(PairArgs p) {
+// A tile of a symmetric matrix as pairs to both sides of the diagonal, from LDS (fp32, tile[t][v]), eight entries of a row at a time.  A
+// tile on the diagonal is taken from where v >= t.
+constexpr int kTileLd = kPairTile + 1;
+__device__ __forceinline__ void pair_store(const float (*tile)[kTileLd], int t0, int v0, half_t* hi, half_t* lo, int ld) {
+#pragma unroll
+    for (int turn = 0; turn < 4; ++turn) {
+        const bool back = turn >= 2;                                 // the mirrored tile: row v0 + r, columns t0 + c ..
+        if (back && t0 == v0) break;
+        const int r = (turn & 1) * 32 + ((int)threadIdx.x >> 3), c = (threadIdx.x & 7) * 8;
+        half8 h, l;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const bool flip = back || (t0 == v0 && c + e < r);
+            const float y = flip ? tile[c + e][r] : tile[r][c + e];
+            h[e] = (half_t)y;
+            l[e] = (half_t)(y - (float)h[e]);
+        }
+        const int64_t to = (int64_t)((back ? v0 : t0) + r) * ld + (back ? t0 : v0) + c;
+        *reinterpret_cast<half8*>(hi + to) = h;
+        *reinterpret_cast<half8*>(lo + to) = l;
+    }
+}
+
+// 64 x 64 tiles, four wavefronts of 32 x 32.  A stage holds 64 of K of both operands' halves, a quarter of it loaded by each wavefront.  Few
+// workgroups keep three stages under way, one to a CU; many one, two to a CU.
+template <PairMode MODE, int STAGES>
+__global__ __launch_bounds__(kPairThreads, STAGES == 2 ? 2 : 1) void ns_pair_kernel(PairArgs p) {
     extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
     constexpr bool kKMajor = MODE == kPairLast;
     int id = ns_by_xcd(blockIdx.x, gridDim.x);
@@ -95,12 +120,15 @@ __global__ __launch_bounds__(kPairThreads, 2) void ns_pair_kernel(PairArgs p) {
         }
     };
     f32x4 acc[2][2] = {}, cross[2][2] = {};
-    issue(first, 0);
+    for (int it = 0; it < STAGES - 1 && it < stages; ++it) issue(first + it, it);
     for (int it = 0; it < stages; ++it) {
-        __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));
-        __syncthreads();                             // this stage is there for everyone, and everyone has left the other one
-        if (it + 1 < stages) issue(first + it + 1, (it + 1) & 1);
-        const unsigned at = (it & 1) * kPairStage;
+        const int behind = min(STAGES - 2, stages - 1 - it);         // stages asked for after this one, eight transfers each
+        if (behind == 0) __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));
+        else if (behind == 1) __builtin_amdgcn_s_waitcnt(vmcnt_imm(8));
+        else __builtin_amdgcn_s_waitcnt(vmcnt_imm(16));
+        __syncthreads();                             // this stage is there for everyone, and everyone has left the one before
+        if (it + STAGES - 1 < stages) issue(first + it + STAGES - 1, (it + STAGES - 1) % STAGES);
+        const unsigned at = it % STAGES * kPairStage;
 #pragma unroll
         for (int k32 = 0; k32 < 2; ++k32) {
             half8 t[2][2], v[2][2];                  // [hi, lo][block]
@@ -119,11 +147,15 @@ __global__ __launch_bounds__(kPairThreads, 2) void ns_pair_kernel(PairArgs p) {
 #pragma unroll
                 for (int tb = 0; tb < 2; ++tb) {
                     acc[vb][tb] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v[0][vb], t[0][tb], acc[vb][tb], 0, 0, 0);
-                    cross[vb][tb] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v[0][vb], t[1][tb], cross[vb][tb], 0, 0, 0);
-                    cross[vb][tb] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v[1][vb], t[0][tb], cross[vb][tb], 0, 0, 0);
+                    f32x4& with_t = MODE == kPairGram ? cross[vb][tb] : acc[vb][tb];           // (X's low halves are scaled)
+                    f32x4& with_v = MODE == kPairGram || MODE == kPairLast ? cross[vb][tb] : acc[vb][tb];
+                    with_t = __builtin_amdgcn_mfma_f32_16x16x32_f16(v[0][vb], t[1][tb], with_t, 0, 0, 0);
+                    with_v = __builtin_amdgcn_mfma_f32_16x16x32_f16(v[1][vb], t[0][tb], with_v, 0, 0, 0);
                 }
         }
     }
+    float(*tile_out)[kTileLd] = reinterpret_cast<float(*)[kTileLd]>(smem);
+    if constexpr (MODE == kPairPoly || MODE == kPairMul) __syncthreads();          // (the stages are read)
 #pragma unroll
     for (int tb = 0; tb < 2; ++tb) {
         const int t = t0 + wt * 32 + tb * 16 + col;
@@ -132,7 +164,8 @@ __global__ __launch_bounds__(kPairThreads, 2) void ns_pair_kernel(PairArgs p) {
             const int v = v0 + wv * 32 + vb * 16 + grp * 4;
             float x[4];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) x[e] = fmaf(cross[vb][tb][e], 1.f / kLoScale, acc[vb][tb][e]);
+            for (int e = 0; e < 4; ++e)
+                x[e] = MODE == kPairGram || MODE == kPairLast ? fmaf(cross[vb][tb][e], 1.f / kLoScale, acc[vb][tb][e]) : acc[vb][tb][e];
             if constexpr (MODE == kPairGram) {
                 *reinterpret_cast<float4*>(p.part + ((int64_t)chunk * p.count + mat) * p.each_out + (int64_t)t * p.ld_out + v) =
                     make_float4(x[0], x[1], x[2], x[3]);
@@ -146,7 +179,6 @@ __global__ __launch_bounds__(kPairThreads, 2) void ns_pair_kernel(PairArgs p) {
                             p.x.out[mat * p.x.each_out + to] = ns_bf16(x[e] * by);
                         }
             } else {
-                half_t *hi = q.out_hi + mat * p.each_out, *lo = q.out_lo + mat * p.each_out;
                 half4 a_hi, a_lo;
                 if constexpr (MODE == kPairPoly) {   // (t_op is A)
                     const int64_t at = mat * p.each_t + (int64_t)t * p.ld_t + v;
@@ -157,167 +189,228 @@ __global__ __launch_bounds__(kPairThreads, 2) void ns_pair_kernel(PairArgs p) {
                 for (int e = 0; e < 4; ++e) {
                     float y = x[e] * q.in_scale;
                     if constexpr (MODE == kPairPoly)
-                        y = fmaf(p.x.c, y, fmaf(p.x.b * (1.f / kOffScale), fmaf((float)a_lo[e], 1.f / kLoScale, (float)a_hi[e]), t == v + e ? p.x.a : 0.f));
-                    y *= q.out_scale;
-                    const half_t h = (half_t)y, l = (half_t)((y - (float)h) * kLoScale);
-                    if (t <= v + e) {
-                        const int64_t to = (int64_t)t * p.ld_out + v + e, back = (int64_t)(v + e) * p.ld_out + t;
-                        hi[to] = h;
-                        lo[to] = l;
-                        hi[back] = h;
-                        lo[back] = l;
-                    }
+                        y = fmaf(p.x.c, y, fmaf(p.x.b * (1.f / kOffScale), (float)a_hi[e] + (float)a_lo[e], t == v + e ? p.x.a : 0.f));
+                    tile_out[t - t0][v - v0 + e] = y * q.out_scale;
                 }
             }
         }
+    }
+    if constexpr (MODE == kPairPoly || MODE == kPairMul) {
+        __syncthreads();
+        pair_store(tile_out, t0, v0, q.out_hi + mat * p.each_out, q.out_lo + mat * p.each_out, p.ld_out);
     }
 }
 
 // A from the partial sums of its tiles, scaled, as pairs on both sides of the diagonal.
 __global__ __launch_bounds__(256) void ns_gather_kernel(const float* part, int chunks, int count, int mp, const float2* scales, half_t* hi, half_t* lo) {
-    const int mat = blockIdx.y, id = blockIdx.x * 256 + threadIdx.x;
-    if (id >= mp * mp) return;
-    const int t = id / mp, v = id - t * mp;
-    if (t > v) return;
-    float x = 0.f;
-    for (int c = 0; c < chunks; ++c) x += part[((int64_t)c * count + mat) * mp * mp + id];
-    x *= scales[mat].x * kOffScale;
-    const half_t h = (half_t)x, l = (half_t)((x - (float)h) * kLoScale);
-    const int64_t to = (int64_t)mat * mp * mp + id, back = (int64_t)mat * mp * mp + v * mp + t;
-    hi[to] = h;
-    lo[to] = l;
-    hi[back] = h;
-    lo[back] = l;
+    __shared__ float tile[kPairTile][kTileLd];
+    const int mat = blockIdx.y;
+    int tile_t, tile_v;
+    pair_tile_at(blockIdx.x, tile_t, tile_v);
+    const int t0 = tile_t * kPairTile, v0 = tile_v * kPairTile;
+    const float by = scales[mat].x * kOffScale;
+#pragma unroll
+    for (int turn = 0; turn < 4; ++turn) {
+        const int r = turn * 16 + ((int)threadIdx.x >> 4), c = (threadIdx.x & 15) * 4;
+        const float* at = part + ((int64_t)mat * mp + t0 + r) * mp + v0 + c;
+        float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+        for (int k = 0; k < chunks; ++k) {
+            const float4 x = *reinterpret_cast<const float4*>(at + (int64_t)k * count * mp * mp);
+            sum.x += x.x; sum.y += x.y; sum.z += x.z; sum.w += x.w;
+        }
+        tile[r][c] = sum.x * by;
+        tile[r][c + 1] = sum.y * by;
+        tile[r][c + 2] = sum.z * by;
+        tile[r][c + 3] = sum.w * by;
+    }
+    __syncthreads();
+    pair_store(tile, t0, v0, hi + (int64_t)mat * mp * mp, lo + (int64_t)mat * mp * mp, mp);
 }
 
-// All steps of one matrix of up to MP = 64 or 128 rows in one workgroup: two matrices in LDS, what becomes of them in registers (16 x 16
-// blocks on one side of the diagonal, dealt out to the wavefronts).
-constexpr int kIterWaves = 16;
+// All steps of one matrix of up to MP = 64 or 128 rows in one workgroup of four wavefronts, each with a strip of columns of every matrix.
+// A block of 16 x 16 comes out of an MFMA as it goes into one: lane l has column l % 16 and rows 4 (l / 16) .. + 3, and two blocks are the
+// 32 of K of the next one's operand, in an order of their own, the same on both sides.  So a strip stays in registers from product to
+// product (M A, then M (M A)); as the matrices are symmetric the other operand, all rows of A or M, is every wavefront's strip as well, and
+// passes through LDS once a step each, in the order of the lanes.  Only the new A is exchanged across the diagonal, where it is
+// made the mean of both sides.
+// Bound by the chain of products: 17 for 5 steps, 24 MFMAs a wavefront each (192 at 128 rows).  64 rows, us: blocks of lower triangles
+// dealt out to 16 wavefronts, mirrored in LDS by pieces of two bytes, 16.5; all blocks where they lie, operands from LDS, 16 wavefronts 20.7,
+// four 26.5.
+constexpr int kIterThreads = 256;
 template <int MP>
-struct IterShape {
-    static constexpr int kSide = MP / 16, kBlocks = kSide * (kSide + 1) / 2, kMine = (kBlocks + kIterWaves - 1) / kIterWaves;
-    static constexpr int kRowBytes = MP * 2, kPieces = MP / 8, kHalf = MP * kRowBytes, kMatrix = 2 * kHalf, kLds = 2 * kMatrix;
-    __device__ static __forceinline__ int at(int r, int c) {                                   // byte of piece c of row r
-        const int swz = MP == 64 ? (r >> 1) & 7 : r & 15;
-        return r * kRowBytes + ((c ^ swz) << 4);
-    }
-};
-template <int MP>
-__global__ __launch_bounds__(kIterWaves * 64) void ns_iterate_kernel(const float* part, int chunks, int count, const float2* scales, int steps,
+__global__ __launch_bounds__(kIterThreads, 1) void ns_iterate_kernel(const float* part, int chunks, int count, const float2* scales, int steps,
                                                                      float a, float b, float c, half_t* p_hi, half_t* p_lo) {
-    typedef IterShape<MP> S;
-    constexpr int kMine = S::kMine;
+    constexpr int kB = MP / 16, kT = MP / 64, kPairs = kB / 2;       // blocks of a column; of a strip's width; operands of 32 of K
+    constexpr int kOperand = kB * kPairs * 2 * 1024, kTurnLd = MP + 1;
     extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
-    unsigned char *const U = smem, *const V = smem + S::kMatrix;
+    unsigned char *const all_m = smem, *const all_a = smem + kOperand;
+    float* const turned = reinterpret_cast<float*>(all_a);           // (MP x kTurnLd, when A has been read)
     const int mat = blockIdx.x, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int col = lane & 15, grp = lane >> 4;
-    int bt[kMine], bv[kMine];
-    bool there[kMine];
-    f32x4 A[kMine], M[kMine], P[kMine];
-    const float by = scales[mat].x;
+    const int col = lane & 15, grp = lane >> 4, strip = wave * kT * 16;
+    typedef f32x4 Strip[kB][kT];
+    struct Pairs {
+        half8 hi[kPairs][kT], lo[kPairs][kT];
+    };
+    Strip A, M, S;
+    Pairs pa, pm, pp;
+    const float by = scales[mat].x * kOffScale;
 #pragma unroll
-    for (int i = 0; i < kMine; ++i) {
-        const int id = wave + i * kIterWaves;
-        there[i] = id < S::kBlocks;
-        pair_tile_at(there[i] ? id : 0, bt[i], bv[i]);
-        A[i] = f32x4{0, 0, 0, 0};
-        M[i] = P[i] = A[i];
-        if (there[i]) {
-            const int64_t at = ((int64_t)mat * MP + bt[i] * 16 + col) * MP + bv[i] * 16 + grp * 4;
-#pragma unroll 4
-            for (int k = 0; k < chunks; ++k) {
-                const float4 x = *reinterpret_cast<const float4*>(part + (int64_t)k * count * MP * MP + at);
-                A[i] += f32x4{x.x, x.y, x.z, x.w};
-            }
-            A[i] *= by;
+    for (int j = 0; j < kB; ++j)
+#pragma unroll
+        for (int i = 0; i < kT; ++i) {
+            const int t = strip + i * 16 + col, v = j * 16 + grp * 4;
+            f32x4 x = {};
+            const float* at = part + (int64_t)mat * MP * MP;         // (there are sums on and above the diagonal)
+            for (int k = 0; k < chunks; ++k, at += (int64_t)count * MP * MP)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) x[e] += at[min(t, v + e) * MP + max(t, v + e)];
+            A[j][i] = x * by;
         }
-    }
-    auto put = [&](unsigned char* to, const f32x4 (&x)[kMine], float scale) {
+    auto split = [&](const Strip& x, Pairs& p) {
+        typedef float f2 __attribute__((ext_vector_type(2)));
+        typedef half_t h2 __attribute__((ext_vector_type(2)));
 #pragma unroll
-        for (int i = 0; i < kMine; ++i)
-            if (there[i]) {
-                const int t = bt[i] * 16 + col;
+        for (int j = 0; j < kB; ++j)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int v = bv[i] * 16 + grp * 4 + e;
-                    const float y = x[i][e] * scale;
-                    const half_t h = (half_t)y, l = (half_t)((y - (float)h) * kLoScale);
-                    if (t <= v) {
-                        const int one = S::at(t, v >> 3) + (v & 7) * 2, other = S::at(v, t >> 3) + (t & 7) * 2;
-                        *reinterpret_cast<half_t*>(to + one) = h;
-                        *reinterpret_cast<half_t*>(to + S::kHalf + one) = l;
-                        *reinterpret_cast<half_t*>(to + other) = h;
-                        *reinterpret_cast<half_t*>(to + S::kHalf + other) = l;
-                    }
+            for (int i = 0; i < kT; ++i)
+#pragma unroll
+                for (int e = 0; e < 4; e += 2) {
+                    const f2 y = {x[j][i][e], x[j][i][e + 1]};
+                    const h2 h = __builtin_convertvector(y, h2);
+                    const f2 rest = {y[0] - (float)h[0], y[1] - (float)h[1]};
+                    const h2 l = __builtin_convertvector(rest, h2);
+                    const int at = (j & 1) * 4 + e;
+                    p.hi[j >> 1][i][at] = h[0];
+                    p.hi[j >> 1][i][at + 1] = h[1];
+                    p.lo[j >> 1][i][at] = l[0];
+                    p.lo[j >> 1][i][at + 1] = l[1];
                 }
-            }
-        __syncthreads();
     };
-    auto product = [&](const unsigned char* v_op, const unsigned char* t_op, f32x4 (&out)[kMine], float scale) {
+    // this strip as rows of the other operand
+    auto publish = [&](unsigned char* all, const Pairs& p) {
 #pragma unroll
-        for (int i = 0; i < kMine; ++i)
-            if (there[i]) {
-                f32x4 acc = {}, cross = {};
-                const int rt = bt[i] * 16 + col, rv = bv[i] * 16 + col;
+        for (int i = 0; i < kT; ++i)
 #pragma unroll
-                for (int k32 = 0; k32 < MP / 32; ++k32) {
-                    const int piece = k32 * 4 + grp;
-                    const half8 th = *reinterpret_cast<const half8*>(t_op + S::at(rt, piece)), tl = *reinterpret_cast<const half8*>(t_op + S::kHalf + S::at(rt, piece));
-                    const half8 vh = *reinterpret_cast<const half8*>(v_op + S::at(rv, piece)), vl = *reinterpret_cast<const half8*>(v_op + S::kHalf + S::at(rv, piece));
-                    acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(vh, th, acc, 0, 0, 0);
-                    cross = __builtin_amdgcn_mfma_f32_16x16x32_f16(vh, tl, cross, 0, 0, 0);
-                    cross = __builtin_amdgcn_mfma_f32_16x16x32_f16(vl, th, cross, 0, 0, 0);
-                }
-                out[i] = (cross * (1.f / kLoScale) + acc) * scale;
+            for (int j = 0; j < kPairs; ++j) {
+                half8* at = reinterpret_cast<half8*>(all + (((wave * kT + i) * kPairs + j) * 2) * 1024) + lane;
+                at[0] = p.hi[j][i];
+                at[64] = p.lo[j][i];
             }
     };
-    constexpr float kOff = kOffScale, kPoly = kPolyScale;
-    put(U, A, kOff);
+    // (chains of MFMAs on one sum side by side: four rows of blocks at a time)
+    auto product = [&](const unsigned char* all, const Pairs& p, Strip& out) {
+#pragma unroll
+        for (int r0 = 0; r0 < kB; r0 += 4) {
+#pragma unroll
+            for (int r = r0; r < r0 + 4; ++r)
+#pragma unroll
+                for (int i = 0; i < kT; ++i) out[r][i] = f32x4{0, 0, 0, 0};
+#pragma unroll
+            for (int j = 0; j < kPairs; ++j) {
+                half8 hi[4], lo[4];
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const half8* at = reinterpret_cast<const half8*>(all + (((r0 + r) * kPairs + j) * 2) * 1024) + lane;
+                    hi[r] = at[0];
+                    lo[r] = at[64];
+                }
+#pragma unroll
+                for (int part = 0; part < 3; ++part)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r)
+#pragma unroll
+                        for (int i = 0; i < kT; ++i)
+                            out[r0 + r][i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(part < 2 ? hi[r] : lo[r], part == 1 ? p.lo[j][i] : p.hi[j][i],
+                                                                                   out[r0 + r][i], 0, 0, 0);
+            }
+        }
+    };
+    // A is held times kOff, P times kPolyScale, M as it is: what M multiplies keeps its scale
+    constexpr float kOff = kOffScale;
+    split(A, pa);
+    publish(all_a, pa);
+    __syncthreads();
     for (int step = 0; step < steps; ++step) {
-        product(U, U, M, 1.f / (kOff * kOff));                       // A A, of A = U
-#pragma unroll
-        for (int i = 0; i < kMine; ++i)
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-                M[i][e] = fmaf(c, M[i][e], fmaf(b, A[i][e], bt[i] * 16 + col == bv[i] * 16 + grp * 4 + e ? a : 0.f));
         const bool last = step + 1 == steps;
-        if (!(last && step == 0)) put(V, M, kOff);
-        if (!last) {
-            f32x4 T[kMine];
-            product(V, U, T, 1.f / (kOff * kOff));                   // M A
-            __syncthreads();
-            put(U, T, kOff);
-            product(V, U, A, 1.f / (kOff * kOff));                   // M A M
-            __syncthreads();
-        }
+        product(all_a, pa, S);
+#pragma unroll
+        for (int j = 0; j < kB; ++j)
+#pragma unroll
+            for (int i = 0; i < kT; ++i)
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    M[j][i][e] = fmaf(c * (1.f / (kOff * kOff)), S[j][i][e],
+                                      fmaf(b * (1.f / kOff), A[j][i][e], strip + i * 16 + col == j * 16 + grp * 4 + e ? a : 0.f));
+        split(M, pm);
+        publish(all_m, pm);
         if (step == 0) {
 #pragma unroll
-            for (int i = 0; i < kMine; ++i) P[i] = M[i];
-        } else {
-            put(U, P, kPoly);
-            product(V, U, P, 1.f / (kOff * kPoly));                  // M P
-            __syncthreads();
+            for (int j = 0; j < kB; ++j)
+#pragma unroll
+                for (int i = 0; i < kT; ++i) M[j][i] *= kPolyScale;
+            split(M, pp);
         }
-        if (!last) put(U, A, kOff);
+        __syncthreads();                                             // all of M is there; A has been read
+        if (step > 0) {
+            product(all_m, pp, S);                                   // M P
+            split(S, pp);
+        }
+        if (last) break;
+        product(all_m, pa, S);                                       // M A
+        split(S, pa);
+        product(all_m, pa, S);                                       // M M A
+#pragma unroll
+        for (int j = 0; j < kB; ++j)
+#pragma unroll
+            for (int i = 0; i < kT; ++i)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) turned[(j * 16 + grp * 4 + e) * kTurnLd + strip + i * 16 + col] = S[j][i][e];
+        __syncthreads();                                             // and M has been read
+#pragma unroll
+        for (int j = 0; j < kB; ++j)
+#pragma unroll
+            for (int i = 0; i < kT; ++i)
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    A[j][i][e] = (S[j][i][e] + turned[(strip + i * 16 + col) * kTurnLd + j * 16 + grp * 4 + e]) * 0.5f;
+        split(A, pa);
+        __syncthreads();
+        publish(all_a, pa);
+        __syncthreads();
     }
 #pragma unroll
-    for (int i = 0; i < kMine; ++i)
-        if (there[i]) {
-            const int t = bt[i] * 16 + col;
+    for (int i = 0; i < kT; ++i)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int v = bv[i] * 16 + grp * 4 + e;
-                const float y = P[i][e] * kPoly;
-                const half_t h = (half_t)y, l = (half_t)((y - (float)h) * kLoScale);
-                if (t <= v) {
-                    const int64_t one = ((int64_t)mat * MP + t) * MP + v, other = ((int64_t)mat * MP + v) * MP + t;
-                    p_hi[one] = h;
-                    p_lo[one] = l;
-                    p_hi[other] = h;
-                    p_lo[other] = l;
-                }
-            }
+        for (int j = 0; j < kB; ++j) {
+            const int64_t at = ((int64_t)mat * MP + strip + i * 16 + col) * MP + j * 16 + grp * 4;
+            const half8 h = pp.hi[j >> 1][i], l = pp.lo[j >> 1][i];
+            *reinterpret_cast<half4*>(p_hi + at) = j & 1 ? half4{h[4], h[5], h[6], h[7]} : half4{h[0], h[1], h[2], h[3]};
+            *reinterpret_cast<half4*>(p_lo + at) = j & 1 ? half4{l[4], l[5], l[6], l[7]} : half4{l[0], l[1], l[2], l[3]};
         }
+}
+
+// Partial sums of many chunks into the first one's place: 64 float4 a workgroup, its four wavefronts a quarter of the chunks each.
+constexpr int kFewChunks = 8;
+__global__ __launch_bounds__(256) void ns_reduce_kernel(float4* part, int chunks, int64_t each) {
+    __shared__ float4 place[4][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t at = (int64_t)blockIdx.x * 64 + lane;
+    float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 8
+    for (int k = wave; k < chunks; k += 4) {
+        const float4 x = part[k * each + at];
+        sum.x += x.x; sum.y += x.y; sum.z += x.z; sum.w += x.w;
+    }
+    place[wave][lane] = sum;
+    __syncthreads();
+    if (wave == 0) {
+        for (int w = 1; w < 4; ++w) {
+            const float4 x = place[w][lane];
+            sum.x += x.x; sum.y += x.y; sum.z += x.z; sum.w += x.w;
+        }
+        part[at] = sum;
+    }
 }
 
 // Whether A, M and P stay within what pairs of fp16 hold at their scales, whatever singular values X begins with, and a^steps, by which
@@ -366,15 +459,21 @@ GramLayout gram_layout(int64_t count, int mp, int np) {
 }
 template <PairMode MODE>
 int launch_pair(PairArgs& p, int problems, hipStream_t s) {
-    hipLaunchKernelGGL(ns_pair_kernel<MODE>, dim3((unsigned)(p.tiles * p.chunks * p.count * problems)), dim3(kPairThreads), 2 * kPairStage, s, p);
+    const unsigned groups = (unsigned)(p.tiles * p.chunks * p.count * problems);
+    if (groups <= kSweepGroups) {
+        if (!allow_lds(reinterpret_cast<const void*>(ns_pair_kernel<MODE, 4>), 4 * kPairStage)) return TPPO_ERR_LAUNCH;
+        hipLaunchKernelGGL((ns_pair_kernel<MODE, 4>), dim3(groups), dim3(kPairThreads), 4 * kPairStage, s, p);
+    } else {
+        hipLaunchKernelGGL((ns_pair_kernel<MODE, 2>), dim3(groups), dim3(kPairThreads), 2 * kPairStage, s, p);
+    }
     return launch_result();
 }
 template <int MP>
 int launch_iterate(const PairArgs& p, half_t* p_hi, half_t* p_lo, hipStream_t s) {
-    if (IterShape<MP>::kLds > 64 * 1024 && !allow_lds(reinterpret_cast<const void*>(ns_iterate_kernel<MP>), IterShape<MP>::kLds))
-        return TPPO_ERR_LAUNCH;
-    hipLaunchKernelGGL(ns_iterate_kernel<MP>, dim3((unsigned)p.count), dim3(kIterWaves * 64), IterShape<MP>::kLds, s, p.part, p.chunks, p.count,
-                       p.scales, p.x.steps, p.x.a, p.x.b, p.x.c, p_hi, p_lo);
+    constexpr int kLds = MP * MP * 4 + MP * (MP + 1) * 4;            // one operand, and the other or A turned round
+    if (kLds > 64 * 1024 && !allow_lds(reinterpret_cast<const void*>(ns_iterate_kernel<MP>), kLds)) return TPPO_ERR_LAUNCH;
+    hipLaunchKernelGGL(ns_iterate_kernel<MP>, dim3((unsigned)p.count), dim3(kIterThreads), kLds, s, p.part, p.chunks, p.count, p.scales,
+                       p.x.steps, p.x.a, p.x.b, p.x.c, p_hi, p_lo);
     return launch_result();
 }
 }  // namespace
@@ -402,12 +501,17 @@ int ns_gram(const NsShape& x, const half_t* hi, const half_t* lo, const float2* 
     p.stages = np / 64;
     p.chunks = L.chunks;
     if (launch_pair<kPairGram>(p, 1, s) != TPPO_OK) return TPPO_ERR_LAUNCH;
+    if (L.chunks > kFewChunks) {
+        const int64_t quads = half / 4;
+        hipLaunchKernelGGL(ns_reduce_kernel, dim3((unsigned)(quads / 64)), dim3(256), 0, s, reinterpret_cast<float4*>(p.part), L.chunks, quads);
+        p.chunks = 1;
+    }
     half_t* P = pair(L.p[0]);
     float p_scale = kPolyScale;
     if (mp <= 128) {
         if ((mp == 64 ? launch_iterate<64>(p, P, P + half, s) : launch_iterate<128>(p, P, P + half, s)) != TPPO_OK) return TPPO_ERR_LAUNCH;
     } else {
-        hipLaunchKernelGGL(ns_gather_kernel, dim3((unsigned)((each + 255) / 256), (unsigned)x.count), dim3(256), 0, s, p.part, p.chunks, p.count, mp,
+        hipLaunchKernelGGL(ns_gather_kernel, dim3((unsigned)L.tiles, (unsigned)x.count), dim3(256), 0, s, p.part, p.chunks, p.count, mp,
                            scales, A, A + half);
         p.chunks = 1;
         p.stages = mp / 64;

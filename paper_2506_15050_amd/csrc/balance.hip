@@ -9,7 +9,7 @@
 
 namespace tppo {
 
-constexpr int kBlThreads = 256, kBlWaves = kBlThreads / kWave;
+constexpr int kBlThreads = 512, kBlWaves = kBlThreads / kWave;
 constexpr int kBlMaxE = 2048, kBlMaxK = 1024;
 constexpr int64_t kBlMaxChoices = (int64_t)1 << 36;  // a workgroup's share of the choices is counted in 32 bits
 constexpr int kBlGroups = 512;                       // workgroups of the rows' kernel at most: rows of partial sums
@@ -65,73 +65,122 @@ struct Balance {
     float* mean_prob;
     float* part_p;                                   // [groups][E]
     int32_t* part_counts;                            // [counters][E]
+    double* part_loss;                               // by workgroup of the finishing kernel
+    int32_t* arrived;                                // how many of those are done; cleared by the kernel before
     int groups, counters;
     int32_t* status;
     __device__ int64_t tokens() const { return m_actual ? max(min(M, *m_actual), (int64_t)0) : M; }
+    __device__ double n_tokens(int64_t m_eff) const { return (double)(denominator > 0 ? denominator : m_eff); }
 };
 
 // This workgroup's share of the choices, token by token, into `seen` (LDS, E words, cleared here).
 __device__ __forceinline__ void count_choices(const Balance& b, int64_t m_eff, int share, int shares, int* seen) {
-    for (int e = threadIdx.x; e < b.E; e += kBlThreads) seen[e] = 0;
+    for (int e = threadIdx.x; e < b.E; e += blockDim.x) seen[e] = 0;
     __syncthreads();
-    const int64_t per = (m_eff + shares - 1) / shares, from = share * per, to = min(from + per, m_eff);
-    const int k = (int)b.k;
-    for (int64_t i = threadIdx.x; i < (to - from) * k; i += kBlThreads) {
-        const int64_t m = from + i / k, row = b.rows ? (int64_t)b.rows[m] : m;
-        if (row < 0 || row >= b.n_rows) {
-            set_status(b.status, TPPO_STATUS_BAD_ROW);
-            continue;
+    const int64_t per = (m_eff + shares - 1) / shares, from = share * per;
+    const int64_t choices = (min(from + per, m_eff) - from) * b.k;
+    const unsigned k = (unsigned)b.k;
+    for (int64_t i0 = 0; i0 < choices; i0 += (int64_t)1 << 30) {     // (in turns that 32 bits number)
+        const unsigned turn = (unsigned)min(choices - i0, (int64_t)1 << 30);
+        const int64_t first = from + i0 / k;
+        const unsigned over = (unsigned)(i0 % k);
+#pragma unroll 4
+        for (unsigned i = threadIdx.x; i < turn; i += blockDim.x) {
+            const unsigned t = (i + over) / k, j = i + over - t * k;
+            const int64_t m = first + t, row = b.rows ? (int64_t)b.rows[m] : m;
+            if (row < 0 || row >= b.n_rows) {
+                set_status(b.status, TPPO_STATUS_BAD_ROW);
+                continue;
+            }
+            const int e = b.experts[row * b.ld_experts + j];
+            if (e >= 0 && e < b.E) atomicAdd(seen + e, 1);
+            else if (e != -1) set_status(b.status, TPPO_STATUS_BAD_TARGET);
         }
-        const int e = b.experts[row * b.ld_experts + i % k];
-        if (e >= 0 && e < b.E) atomicAdd(seen + e, 1);
-        else if (e != -1) set_status(b.status, TPPO_STATUS_BAD_TARGET);
     }
     __syncthreads();
 }
 
-__global__ __launch_bounds__(kBlThreads) void balance_count_kernel(Balance b) {
+constexpr int kBlCountThreads = 1024;
+__global__ __launch_bounds__(kBlCountThreads) void balance_count_kernel(Balance b) {
     __shared__ int seen[kBlMaxE];
     count_choices(b, b.tokens(), blockIdx.x, b.counters, seen);
-    for (int e = threadIdx.x; e < b.E; e += kBlThreads) b.part_counts[(int64_t)blockIdx.x * b.E + e] = seen[e];
+    for (int e = threadIdx.x; e < b.E; e += kBlCountThreads) b.part_counts[(int64_t)blockIdx.x * b.E + e] = seen[e];
 }
 
-// kLanes lanes a row, kPieces pieces of 16 bytes for each.  GRAD: counts are there already, and derivatives are written; otherwise the
-// workgroup counts its part of the choices as well.
-template <class T, int kLanes, int kPieces, bool RAGGED, bool GRAD>
+// A sum over the workgroup, in every thread (kBlThreads of them).
+__device__ __forceinline__ double workgroup_sum(double x, double* place) {
+    x = wave_prefix(x);
+    if ((threadIdx.x & 63) == 63) place[threadIdx.x >> 6] = x;
+    __syncthreads();
+    x = 0.0;
+#pragma unroll
+    for (int w = 0; w < kBlWaves; ++w) x += place[w];
+    __syncthreads();
+    return x;
+}
+
+// kLanes lanes a row, kPieces pieces of 16 bytes for each, kAtOnce rows under way.  GRAD: derivatives are written, from counts that are
+// there already; otherwise the workgroup counts its part of the choices as well.  ONE: a single workgroup, which does all of the call.
+// Sums over a row are log2(kLanes) steps for 64 / kLanes rows side by side, so lanes are few and have several pieces as long as registers
+// for the columns' sums and counts (2 kPieces kN) are no matter.
+template <class T, int kLanes, int kPieces, bool RAGGED, bool GRAD, bool ONE>
 __global__ __launch_bounds__(kBlThreads) void balance_rows_kernel(Balance b) {
-    constexpr int kN = Piece<T>::kN, kRows = kBlThreads / kLanes;
+    constexpr int kN = Piece<T>::kN, kRows = kBlThreads / kLanes, kAtOnce = kPieces * kN <= 16 ? 2 : 1;
     constexpr int kCols = kLanes * kPieces * kN;
-    __shared__ float columns[kCols * kBlWaves];
-    __shared__ int seen[GRAD ? 1 : kBlMaxE];
+    // the columns' sums wavefront by wavefront (in two turns where that is much)
+    constexpr int kTurns = kCols * kBlWaves * 4 > 32768 ? 2 : 1, kPlaces = kBlWaves / kTurns;
+    __shared__ float columns[kCols * kPlaces > kBlMaxE ? kCols * kPlaces : kBlMaxE];
+    __shared__ int seen[GRAD && !ONE ? 1 : kBlMaxE];
+    __shared__ double sums[kBlWaves];
     const int lane = threadIdx.x % kLanes, mine = threadIdx.x / kLanes, E = b.E;
     const int64_t m_eff = b.tokens();
     const int pieces = (E + kN - 1) / kN;
+    if (!ONE && blockIdx.x == 0 && threadIdx.x == 0) *b.arrived = 0;
     float d[kPieces][kN], total[kPieces][kN];
 #pragma unroll
     for (int i = 0; i < kPieces; ++i)
 #pragma unroll
         for (int e = 0; e < kN; ++e) d[i][e] = total[i][e] = 0.f;
     float up = 0.f;
+    if constexpr (!GRAD || ONE) {
+        count_choices(b, m_eff, blockIdx.x, b.groups, seen);
+        if constexpr (!ONE)
+            for (int e = threadIdx.x; e < E; e += kBlThreads) b.part_counts[(int64_t)blockIdx.x * E + e] = seen[e];
+    }
     if constexpr (GRAD) {
-        const double n = (double)(b.denominator > 0 ? b.denominator : m_eff), each = 1.0 / ((double)b.k * n);
+        const double n = b.n_tokens(m_eff), each = 1.0 / ((double)b.k * n);
         up = (float)((double)b.scale * b.coefficient * E / n);
-        // all counts, and their sum
+        // all counts, and their sum: a column to a thread, or its parts to several
         double sum = 0.0;
-        for (int e = threadIdx.x; e < E; e += kBlThreads) {
-            int64_t c = 0;
-            if (b.counts_in) c = b.counts_in[e];
-            else
-                for (int g = 0; g < b.counters; ++g) c += b.part_counts[(int64_t)g * E + e];
-            columns[e] = (float)((double)c * each);
-            sum += (double)c;
+        if (b.counts_in || ONE) {
+            for (int e = threadIdx.x; e < E; e += kBlThreads) {
+                const double c = b.counts_in ? (double)b.counts_in[e] : (double)seen[e];
+                columns[e] = (float)(c * each);
+                sum += c;
+            }
+        } else {
+            int* parts = reinterpret_cast<int*>(columns);
+            const int width = E <= 64 ? 64 : E <= 128 ? 128 : E <= 256 ? 256 : kBlThreads, shares = kBlThreads / width;
+            const int at = threadIdx.x % width, share = threadIdx.x / width;
+            for (int e0 = 0; e0 < E; e0 += width) {
+                int c = 0;
+                if (e0 + at < E)
+#pragma unroll 16
+                    for (int g = share; g < b.counters; g += shares) c += b.part_counts[(int64_t)g * E + e0 + at];
+                if (shares > 1) {                                    // (then this is the only turn)
+                    parts[threadIdx.x] = c;
+                    __syncthreads();
+                    if (share == 0)
+                        for (int w = 1; w < shares; ++w) c += parts[w * width + at];
+                    __syncthreads();
+                }
+                if (share == 0 && e0 + at < E) {
+                    columns[e0 + at] = (float)((double)c * each);
+                    sum += (double)c;
+                }
+            }
         }
-        __shared__ double sums[kBlWaves];
-        sum = wave_prefix(sum);
-        if ((threadIdx.x & 63) == 63) sums[threadIdx.x >> 6] = sum;
-        __syncthreads();
-        sum = 0.0;
-#pragma unroll
-        for (int w = 0; w < kBlWaves; ++w) sum += sums[w];
+        sum = workgroup_sum(sum, sums);
         const float mean = (float)(sum * each / E);
 #pragma unroll
         for (int i = 0; i < kPieces; ++i)
@@ -141,65 +190,74 @@ __global__ __launch_bounds__(kBlThreads) void balance_rows_kernel(Balance b) {
                 d[i][e] = at < E ? columns[at] - mean : 0.f;
             }
         __syncthreads();
-    } else {
-        count_choices(b, m_eff, blockIdx.x, b.groups, seen);
-        for (int e = threadIdx.x; e < E; e += kBlThreads) b.part_counts[(int64_t)blockIdx.x * E + e] = seen[e];
     }
-    for (int64_t m = (int64_t)blockIdx.x * kRows + mine; m < m_eff; m += (int64_t)b.groups * kRows) {
-        const int64_t want = b.rows ? (int64_t)b.rows[m] : m;
-        const bool bad = want < 0 || want >= b.n_rows;
-        const T* src = static_cast<const T*>(b.logits) + (bad ? 0 : want) * b.ld;
-        float z[kPieces][kN], top = -INFINITY;
+    const int64_t stride = (int64_t)b.groups * kRows;
+    for (int64_t m0 = (int64_t)blockIdx.x * kRows + mine; m0 < m_eff; m0 += stride * kAtOnce) {
+        Piece<T> p[kAtOnce][kPieces];
+        bool bad[kAtOnce];
 #pragma unroll
-        for (int i = 0; i < kPieces; ++i) {
-            const int c = lane + i * kLanes;
-            Piece<T> p;
-            if (c < pieces) p = piece_at<T, RAGGED>(src, c, E, -INFINITY);
+        for (int a = 0; a < kAtOnce; ++a) {
+            const int64_t m = min(m0 + a * stride, m_eff - 1);      // (beyond the end: the last one again, not used)
+            const int64_t want = b.rows ? (int64_t)b.rows[m] : m;
+            bad[a] = want < 0 || want >= b.n_rows;
+            const T* src = static_cast<const T*>(b.logits) + (bad[a] ? 0 : want) * b.ld;
 #pragma unroll
-            for (int e = 0; e < kN; ++e) {
-                z[i][e] = c < pieces ? p.get(e) : -INFINITY;
-                top = fmaxf(top, z[i][e]);
-            }
+            for (int i = 0; i < kPieces; ++i)
+                if (lane + i * kLanes < pieces) p[a][i] = piece_at<T, RAGGED>(src, lane + i * kLanes, E, -INFINITY);
         }
-        top = over_lanes<1, kLanes>(top, Max());
-        if (top == -INFINITY) top = 0.f;                             // nothing to choose from: every exp is 0
-        float sum = 0.f;
 #pragma unroll
-        for (int i = 0; i < kPieces; ++i)
+        for (int a = 0; a < kAtOnce; ++a) {
+            const int64_t m = m0 + a * stride;
+            if (m >= m_eff) break;
+            float z[kPieces][kN], top = -INFINITY;
 #pragma unroll
-            for (int e = 0; e < kN; ++e) {
-                z[i][e] = __builtin_amdgcn_exp2f((z[i][e] - top) * 1.4426950408889634f);
-                sum += z[i][e];
-            }
-        sum = over_lanes<1, kLanes>(sum, Sum());
-        const float inv = sum == 0.f ? 0.f : 1.f / sum;
-        float mean = 0.f;
+            for (int i = 0; i < kPieces; ++i)
 #pragma unroll
-        for (int i = 0; i < kPieces; ++i)
+                for (int e = 0; e < kN; ++e) {
+                    z[i][e] = lane + i * kLanes < pieces ? p[a][i].get(e) : -INFINITY;
+                    top = fmaxf(top, z[i][e]);
+                }
+            top = over_lanes<1, kLanes>(top, Max());
+            if (top == -INFINITY) top = 0.f;                         // nothing to choose from: every exp is 0
+            float sum = 0.f;
 #pragma unroll
-            for (int e = 0; e < kN; ++e) {
-                z[i][e] *= inv;
-                if (!bad) total[i][e] += z[i][e];
-                if constexpr (GRAD) mean = fmaf(z[i][e], d[i][e], mean);
-            }
-        if (bad && lane == 0) set_status(b.status, TPPO_STATUS_BAD_ROW);
-        if constexpr (GRAD) {
-            mean = over_lanes<1, kLanes>(mean, Sum());
-            const float by = bad ? __builtin_nanf("") : up;
-            const int64_t to = b.out_index ? (int64_t)b.out_index[m] : m;
-            if (to < 0 || to >= b.n_out) {
-                if (lane == 0) set_status(b.status, TPPO_STATUS_BAD_ROW);
-                continue;
-            }
-            T* dst = static_cast<T*>(b.grad) + to * b.ld_grad;
+            for (int i = 0; i < kPieces; ++i)
 #pragma unroll
-            for (int i = 0; i < kPieces; ++i) {
-                const int c = lane + i * kLanes;
-                if (c < pieces) {
-                    float out[kN];
+                for (int e = 0; e < kN; ++e) {
+                    z[i][e] = __builtin_amdgcn_exp2f((z[i][e] - top) * 1.4426950408889634f);
+                    sum += z[i][e];
+                }
+            sum = over_lanes<1, kLanes>(sum, Sum());
+            const float inv = sum == 0.f || bad[a] ? 0.f : 1.f / sum;
+            float mean = 0.f;
 #pragma unroll
-                    for (int e = 0; e < kN; ++e) out[e] = by * z[i][e] * (d[i][e] - mean);
-                    put_piece<T, kN, RAGGED>(dst, c, E, out);
+            for (int i = 0; i < kPieces; ++i)
+#pragma unroll
+                for (int e = 0; e < kN; ++e) {
+                    if (bad[a]) z[i][e] = 0.f;                       // (whatever row 0 holds)
+                    z[i][e] *= inv;
+                    total[i][e] += z[i][e];
+                    if constexpr (GRAD) mean = fmaf(z[i][e], d[i][e], mean);
+                }
+            if (bad[a] && lane == 0) set_status(b.status, TPPO_STATUS_BAD_ROW);
+            if constexpr (GRAD) {
+                mean = over_lanes<1, kLanes>(mean, Sum());
+                const float by = bad[a] ? __builtin_nanf("") : up;
+                const int64_t to = b.out_index ? (int64_t)b.out_index[m] : m;
+                if (to < 0 || to >= b.n_out) {
+                    if (lane == 0) set_status(b.status, TPPO_STATUS_BAD_ROW);
+                } else {
+                    T* dst = static_cast<T*>(b.grad) + to * b.ld_grad;
+#pragma unroll
+                    for (int i = 0; i < kPieces; ++i) {
+                        const int c = lane + i * kLanes;
+                        if (c < pieces) {
+                            float out[kN];
+#pragma unroll
+                            for (int e = 0; e < kN; ++e) out[e] = by * z[i][e] * (d[i][e] - mean);
+                            put_piece<T, kN, RAGGED>(dst, c, E, out);
+                        }
+                    }
                 }
             }
         }
@@ -208,64 +266,88 @@ __global__ __launch_bounds__(kBlThreads) void balance_rows_kernel(Balance b) {
 #pragma unroll
     for (int i = 0; i < kPieces; ++i)
 #pragma unroll
-        for (int e = 0; e < kN; ++e) {
-            const float t = over_lanes<kLanes, 64>(total[i][e], Sum());
-            if ((threadIdx.x & 63) < kLanes) columns[(threadIdx.x >> 6) * kCols + (lane + i * kLanes) * kN + e] = t;
-        }
-    __syncthreads();
+        for (int e = 0; e < kN; ++e) total[i][e] = over_lanes<kLanes, 64>(total[i][e], Sum());
+    const int wave = threadIdx.x >> 6;
+#pragma unroll
+    for (int turn = kTurns - 1; turn >= 0; --turn) {                 // (the second half of the wavefronts first, then added to the first)
+        if (wave / kPlaces == turn && (threadIdx.x & 63) < kLanes)
+#pragma unroll
+            for (int i = 0; i < kPieces; ++i)
+#pragma unroll
+                for (int e = 0; e < kN; ++e) {
+                    float* at = columns + (wave % kPlaces) * kCols + (lane + i * kLanes) * kN + e;
+                    *at = turn + 1 < kTurns ? *at + total[i][e] : total[i][e];
+                }
+        __syncthreads();
+    }
+    double loss = 0.0;
+    const double n = b.n_tokens(m_eff);
     for (int e = threadIdx.x; e < E; e += kBlThreads) {
         float t = 0.f;
 #pragma unroll
-        for (int w = 0; w < kBlWaves; ++w) t += columns[w * kCols + e];
-        b.part_p[(int64_t)blockIdx.x * E + e] = t;
+        for (int w = 0; w < kPlaces; ++w) t += columns[w * kCols + e];
+        if constexpr (ONE) {
+            const double q = n > 0.0 ? (double)t / n : 0.0;
+            if (b.counts) b.counts[e] = seen[e];
+            if (b.mean_prob) b.mean_prob[e] = (float)q;
+            if (n > 0.0) loss += (double)(b.counts_in ? b.counts_in[e] : (int64_t)seen[e]) / ((double)b.k * n) * q;
+        } else {
+            b.part_p[(int64_t)blockIdx.x * E + e] = t;
+        }
+    }
+    if constexpr (ONE) {
+        loss = workgroup_sum(loss, sums);
+        if (threadIdx.x == 0 && b.loss) *b.loss = (float)((double)b.coefficient * E * loss);
     }
 }
 
-// Counts, mean probabilities and the loss from the partial sums: one workgroup, a column to a thread of each of its parts.
-constexpr int kBlLast = 1024;
+// Counts, mean probabilities and the loss from the partial sums: kBlColumns columns a workgroup, 32 threads to each.  The last workgroup to
+// end adds up the losses of all, in their order.
+constexpr int kBlLast = 1024, kBlColumns = 32, kBlShares = kBlLast / kBlColumns;
 __global__ __launch_bounds__(kBlLast) void balance_finish_kernel(Balance b) {
-    __shared__ double shares[kBlLast];
-    __shared__ long long chosen[kBlLast];
-    const int E = b.E;
-    const int64_t m_eff = b.tokens();
-    const double n = (double)(b.denominator > 0 ? b.denominator : m_eff);
-    int width = 1;
-    while (width < E && width < kBlLast) width *= 2;
-    const int parts = kBlLast / width, part = threadIdx.x / width, at = threadIdx.x % width;
+    __shared__ double shares[kBlShares][kBlColumns + 1];
+    __shared__ long long chosen[kBlShares][kBlColumns + 1];
+    const int E = b.E, at = threadIdx.x % kBlColumns, share = threadIdx.x / kBlColumns, e = blockIdx.x * kBlColumns + at;
+    double p = 0.0;
+    long long c = 0;
+    if (e < E) {
+#pragma unroll 16
+        for (int g = share; g < b.groups; g += kBlShares) p += (double)b.part_p[(int64_t)g * E + e];
+#pragma unroll 16
+        for (int g = share; g < b.counters; g += kBlShares) c += b.part_counts[(int64_t)g * E + e];
+    }
+    shares[share][at] = p;
+    chosen[share][at] = c;
+    __syncthreads();
+    if (threadIdx.x >= kWave) return;
     double loss = 0.0;
-    for (int e0 = 0; e0 < E; e0 += width) {
-        const int e = e0 + at;
-        double p = 0.0;
-        long long c = 0;
-        if (e < E) {
-            for (int g = part; g < b.groups; g += parts) p += (double)b.part_p[(int64_t)g * E + e];
-            for (int g = part; g < b.counters; g += parts) c += b.part_counts[(int64_t)g * E + e];
+    if (threadIdx.x < kBlColumns && e < E) {
+        const double n = b.n_tokens(b.tokens());
+#pragma unroll 8
+        for (int s = 1; s < kBlShares; ++s) {
+            p += shares[s][at];
+            c += chosen[s][at];
         }
-        shares[threadIdx.x] = p;
-        chosen[threadIdx.x] = c;
-        __syncthreads();
-        if (part == 0 && e < E) {
-            for (int s = 1; s < parts; ++s) {
-                p += shares[s * width + at];
-                c += chosen[s * width + at];
-            }
-            p = n > 0.0 ? p / n : 0.0;
-            if (b.counts) b.counts[e] = c;
-            if (b.mean_prob) b.mean_prob[e] = (float)p;
-            const double all = (double)(b.counts_in ? b.counts_in[e] : c);
-            if (n > 0.0) loss += all / ((double)b.k * n) * p;
-        }
-        __syncthreads();
+        p = n > 0.0 ? p / n : 0.0;
+        if (b.counts) b.counts[e] = c;
+        if (b.mean_prob) b.mean_prob[e] = (float)p;
+        if (n > 0.0) loss = (double)(b.counts_in ? b.counts_in[e] : (int64_t)c) / ((double)b.k * n) * p;
     }
     loss = wave_prefix(loss);
-    if ((threadIdx.x & 63) == 63) shares[threadIdx.x >> 6] = loss;
-    __syncthreads();
-    if (threadIdx.x == 0 && b.loss) {
-        double all = 0.0;
-        for (int w = 0; w < kBlLast / kWave; ++w) all += shares[w];
-        *b.loss = (float)((double)b.coefficient * E * all);
+    if (threadIdx.x == kWave - 1 && b.loss) {
+        __hip_atomic_store(b.part_loss + blockIdx.x, loss, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        __threadfence();
+        if (atomicAdd(b.arrived, 1) + 1 == (int)gridDim.x) {
+            __threadfence();
+            double all = 0.0;
+            for (int w = 0; w < (int)gridDim.x; ++w) all += __hip_atomic_load(b.part_loss + w, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            *b.loss = (float)((double)b.coefficient * E * all);
+        }
     }
 }
+
+// Lanes of a row for so many pieces: 4, 8 or 16, and 64 beyond 64 pieces.
+static int lanes_of(int64_t pieces) { return pieces <= 4 ? 4 : pieces <= 8 ? 8 : pieces <= 64 ? 16 : 64; }
 
 template <class T, bool GRAD>
 static void launch_rows(const Balance& b, hipStream_t s) {
@@ -273,28 +355,39 @@ static void launch_rows(const Balance& b, hipStream_t s) {
     const int pieces = (b.E + kN - 1) / kN;
     auto go = [&](auto lanes, auto n) {
         constexpr int kLanes = decltype(lanes)::value, kPieces = decltype(n)::value;
-        if (b.E % kN) hipLaunchKernelGGL((balance_rows_kernel<T, kLanes, kPieces, true, GRAD>), dim3(b.groups), dim3(kBlThreads), 0, s, b);
-        else hipLaunchKernelGGL((balance_rows_kernel<T, kLanes, kPieces, false, GRAD>), dim3(b.groups), dim3(kBlThreads), 0, s, b);
+        auto launch = [&](auto ragged, auto one) {
+            hipLaunchKernelGGL((balance_rows_kernel<T, kLanes, kPieces, decltype(ragged)::value, GRAD, decltype(one)::value>), dim3(b.groups),
+                               dim3(kBlThreads), 0, s, b);
+        };
+        auto sized = [&](auto ragged) {
+            if (b.groups == 1) launch(ragged, std::true_type());
+            else launch(ragged, std::false_type());
+        };
+        if (b.E % kN) sized(std::true_type());
+        else sized(std::false_type());
     };
     typedef std::integral_constant<int, 1> One;
+    typedef std::integral_constant<int, 2> Two;
+    typedef std::integral_constant<int, 4> Four;
+    typedef std::integral_constant<int, 16> Row;
     typedef std::integral_constant<int, 64> Wave;
-    if (pieces <= 4) go(std::integral_constant<int, 4>(), One());
+    if (pieces <= 4) go(Four(), One());
     else if (pieces <= 8) go(std::integral_constant<int, 8>(), One());
-    else if (pieces <= 16) go(std::integral_constant<int, 16>(), One());
-    else if (pieces <= 32) go(std::integral_constant<int, 32>(), One());
-    else if (pieces <= 64) go(Wave(), One());
-    else if (pieces <= 128) go(Wave(), std::integral_constant<int, 2>());
-    else if (pieces <= 256) go(Wave(), std::integral_constant<int, 4>());
+    else if (pieces <= 16) go(Row(), One());
+    else if (pieces <= 32) go(Row(), Two());
+    else if (pieces <= 64) go(Row(), Four());
+    else if (pieces <= 128) go(Wave(), Two());
+    else if (pieces <= 256) go(Wave(), Four());
     else if constexpr (kN == 4) go(Wave(), std::integral_constant<int, 8>());
 }
 
-// Workgroups of the rows' kernel: as many as have a row to each group of lanes, up to kBlGroups.
-static int row_groups(int64_t M, int64_t E, int per_piece) {
-    const int64_t pieces = (E + per_piece - 1) / per_piece;
-    int64_t lanes = 4;
-    while (lanes < pieces && lanes < 64) lanes *= 2;
-    const int64_t rows = kBlThreads / lanes, want = (M + rows - 1) / rows;
-    return (int)(want < 1 ? 1 : want < kBlGroups ? want : kBlGroups);
+// Workgroups of the rows' kernel: up to kBlGroups, as many as have rows for all their lanes; one alone where that has no more than
+// kBlAlone pieces a thread and so many choices, whose work is less than the two or three launches that it does without.
+constexpr int64_t kBlAlone = 8;
+static int row_groups(int64_t M, int64_t k, int64_t E, int per_piece) {
+    const int64_t pieces = (E + per_piece - 1) / per_piece, rows = kBlThreads / lanes_of(pieces), want = (M + rows - 1) / rows;
+    if (M * pieces <= kBlAlone * kBlThreads && M * k <= kBlAlone * kBlThreads) return 1;
+    return (int)(want < 2 ? 2 : want < kBlGroups ? want : kBlGroups);
 }
 
 static int check(const Balance& b, tppo_dtype dt) {
@@ -318,21 +411,27 @@ static size_t part_bytes(int64_t E, int rows) { return round_up((size_t)rows * E
 static int run_balance(Balance& b, tppo_dtype dt, bool grad, void* workspace, size_t workspace_bytes, hipStream_t s) {
     if (!workspace || !is_aligned(workspace, 256) || workspace_bytes < tppo_balance_loss_workspace_bytes(b.M, b.E))
         return TPPO_ERR_WORKSPACE;
-    b.groups = row_groups(b.M, b.E, dt == TPPO_F32 ? 4 : 8);
-    b.part_p = static_cast<float*>(workspace);
-    b.part_counts = reinterpret_cast<int32_t*>(static_cast<char*>(workspace) + part_bytes(b.E, kBlGroups));
+    b.groups = row_groups(b.M, b.k, b.E, dt == TPPO_F32 ? 4 : 8);
+    char* ws = static_cast<char*>(workspace);
+    b.part_p = reinterpret_cast<float*>(ws);
+    b.part_counts = reinterpret_cast<int32_t*>(ws + part_bytes(b.E, kBlGroups));
+    b.part_loss = reinterpret_cast<double*>(ws + 2 * part_bytes(b.E, kBlGroups));
+    b.arrived = reinterpret_cast<int32_t*>(b.part_loss + kBlMaxE / kBlColumns);
+    b.counters = b.groups;
     if (grad) {
-        const int64_t want = (b.M * b.k + 4 * kBlThreads - 1) / (4 * kBlThreads);
-        b.counters = (int)(want < 1 ? 1 : want < kBlCounters ? want : kBlCounters);
-        hipLaunchKernelGGL(balance_count_kernel, dim3(b.counters), dim3(kBlThreads), 0, s, b);
+        if (b.groups > 1) {
+            const int64_t want = (b.M * b.k + 4 * kBlCountThreads - 1) / (4 * kBlCountThreads);
+            b.counters = (int)(want < 1 ? 1 : want < kBlCounters ? want : kBlCounters);
+            hipLaunchKernelGGL(balance_count_kernel, dim3(b.counters), dim3(kBlCountThreads), 0, s, b);
+        }
         if (dt == TPPO_F32) launch_rows<float, true>(b, s);
         else launch_rows<uint16_t, true>(b, s);
     } else {
-        b.counters = b.groups;
         if (dt == TPPO_F32) launch_rows<float, false>(b, s);
         else launch_rows<uint16_t, false>(b, s);
     }
-    hipLaunchKernelGGL(balance_finish_kernel, dim3(1), dim3(kBlLast), 0, s, b);
+    if (b.groups > 1)
+        hipLaunchKernelGGL(balance_finish_kernel, dim3((b.E + kBlColumns - 1) / kBlColumns), dim3(kBlLast), 0, s, b);
     return launch_result();
 }
 
@@ -342,7 +441,7 @@ extern "C" size_t tppo_balance_loss_workspace_bytes(int64_t M, int64_t E) {
     using namespace tppo;
     (void)M;
     if (E < 1 || E > kBlMaxE) return 256;
-    return 2 * part_bytes(E, kBlGroups);
+    return 2 * part_bytes(E, kBlGroups) + round_up((kBlMaxE / kBlColumns) * sizeof(double) + sizeof(int32_t), 256);
 }
 
 extern "C" int tppo_balance_loss(const void* logits, int64_t n_rows, int64_t E, int64_t ld, tppo_dtype dt, const int32_t* experts,

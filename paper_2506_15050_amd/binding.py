@@ -132,6 +132,8 @@ if hasattr(torch._C, "_cuda_getCurrentRawStream") and hasattr(torch._C, "_cuda_g
     def _stream():
         return _raw_stream(_device())
 else:
+    _device = torch.cuda.current_device
+
     def _stream():
         return torch.cuda.current_stream().cuda_stream
 
@@ -354,75 +356,25 @@ def tppo_value_head(hidden, w_value, bias=0.0, rows=None, M=None, m_actual=None,
     return v
 
 
-_DTYPES = {torch.float32: TPPO_F32, torch.bfloat16: TPPO_BF16}
-
-
-def _rows_like(t, what):
-    """A device matrix whose rows lie whole in memory, for a call that takes their stride."""
-    if not (t.is_cuda and t.dim() == 2 and t.dtype in _DTYPES and (t.stride(1) == 1 or t.shape[1] == 1)):
-        raise ValueError(f"{what}: a device matrix of fp32 or bf16 with rows contiguous in memory is required")
-    return t, (t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1]))
-
-
-def _vector_like(t, n, dtypes, what):
-    """A contiguous device tensor of n elements (None passes)."""
-    if t is None:
-        return None
-    if not (t.is_cuda and t.is_contiguous() and t.numel() == n and t.dtype in dtypes):
-        raise ValueError(f"{what}: a contiguous device tensor of {n} elements of the documented type is required")
-    return t
-
-
-def _count_rows(rows, M, n_rows, what):
-    """The number of rows a call is about, and its list checked against it."""
-    if rows is not None:
-        if not (rows.is_cuda and rows.dtype == torch.int32 and rows.is_contiguous()):
-            raise ValueError(f"{what}: rows must be a contiguous int32 device tensor")
-        if M is not None and int(M) > rows.numel():
-            raise ValueError(f"{what}: M = {int(M)} is more than the {rows.numel()} rows listed")
-        return rows.numel() if M is None else int(M)
-    return n_rows if M is None else int(M)
-
-
-def _same_device(what, first, *others):
-    for t in others:
-        if t is not None and t.device != first.device:
-            raise ValueError(f"{what}: tensors on {first.device} and {t.device}")
-
-
-def _m_actual(t, what):
-    if t is not None and not (t.is_cuda and t.dtype == torch.int64 and t.numel() >= 1):
-        raise ValueError(f"{what}: m_actual must be an int64 device tensor")
-    return t
+def _there(call, first, what, *arguments):
+    """A call of the native half, with `first` and the other arguments and the stream, on the device that `first` is on."""
+    device = first.get_device() if isinstance(first, torch.Tensor) else -1
+    if device < 0:
+        raise ValueError(f"{what}: device tensors are required")
+    if device == _device():
+        made = call(first, *arguments, _stream())
+    else:
+        with torch.cuda.device(device):
+            made = call(first, *arguments, _stream())
+    if made.__class__ is int:
+        _check(made, what)
+    return made
 
 
 def tppo_layer_norm(x, weight, bias=None, eps=1e-5, rows=None, M=None, m_actual=None, want_stats=True, status=None, out=None):
     """Layer norm of the rows x[rows] (rows None: all), compact.  x [n_rows, H] bf16 or fp32; weight, bias [H] fp32, or bf16
     with bf16 x.  ``out``: (y, mean, rstd) to write to.  Returns (y, mean, rstd); the statistics are None without ``want_stats``."""
-    what = "tppo_layer_norm"
-    lib = load()
-    x, ld_x = _rows_like(x, what)
-    n_rows, H = x.shape
-    M = _count_rows(rows, M, n_rows, what)
-    _vector_like(weight, H, _DTYPES, what)
-    _vector_like(bias, H, (weight.dtype,), what)
-    if out is None:
-        y = torch.empty(M, H, dtype=x.dtype, device=x.device)
-        mean, rstd = (torch.empty(M, dtype=torch.float32, device=x.device) for _ in range(2)) if want_stats else (None, None)
-    else:
-        y, mean, rstd = out
-        for t in (mean, rstd):
-            _vector_like(t, t.numel() if t is not None and t.numel() >= M else M, (torch.float32,), what)
-    y, ld_y = _rows_like(y, what)
-    if y.dtype != x.dtype or y.shape[0] < M or y.shape[1] != H:
-        raise ValueError(f"{what}: y must be [M, H] of x's type")
-    _same_device(what, x, weight, bias, rows, y, mean, rstd, _m_actual(m_actual, what), status)
-    with torch.cuda.device(x.device):
-        rc = lib.tppo_layer_norm(_ptr(x), n_rows, H, ld_x, _DTYPES[x.dtype], _ptr(weight), _ptr(bias), _DTYPES[weight.dtype],
-                                 float(eps), _ptr(rows), M, _ptr(m_actual), _ptr(y), ld_y, _ptr(mean), _ptr(rstd), _ptr(status),
-                                 _stream())
-    _check(rc, what)
-    return y, mean, rstd
+    return _there(_native().layer_norm, x, "tppo_layer_norm", weight, bias, eps, rows, M, m_actual, want_stats, status, out)
 
 
 def tppo_layer_norm_backward(grad_y, x, weight, mean, rstd, rows=None, M=None, m_actual=None, out_index=None, out=None,
@@ -432,90 +384,18 @@ def tppo_layer_norm_backward(grad_y, x, weight, mean, rstd, rows=None, M=None, m
     write to, whose rows ``out_index`` names (None: 0 .. M-1); otherwise a new [M, H] one of ``grad_dtype`` (x's by default).
     ``grad_w``: (grad_weight, grad_bias) fp32 to write, or with ``accumulate_w`` to add, to.  Returns (grad_x, grad_weight,
     grad_bias), None where not wanted."""
-    what = "tppo_layer_norm_backward"
-    lib = load()
-    x, ld_x = _rows_like(x, what)
-    grad_y, ld_gy = _rows_like(grad_y, what)
-    n_rows, H = x.shape
-    M = _count_rows(rows, M, n_rows, what)
-    if grad_y.shape[0] < M or grad_y.shape[1] != H:
-        raise ValueError(f"{what}: grad_y must be [M, H]")
-    _vector_like(weight, H, _DTYPES, what)
-    for t in (mean, rstd):
-        if t.numel() < M:
-            raise ValueError(f"{what}: statistics of {M} rows are required")
-        _vector_like(t, t.numel(), (torch.float32,), what)
-    if out_index is not None and not (out_index.is_cuda and out_index.dtype == torch.int32 and out_index.is_contiguous() and
-                                      out_index.numel() >= M):
-        raise ValueError(f"{what}: out_index must be a contiguous int32 device tensor of M entries")
-    if out_index is not None and out is None and want_x:
-        raise ValueError(f"{what}: out_index needs the tensor that it points into (out)")
-    gx, ld_gx = None, H
-    if want_x:
-        gx = torch.empty(M, H, dtype=grad_dtype or x.dtype, device=x.device) if out is None else out
-        gx, ld_gx = _rows_like(gx, what)
-        if gx.shape[1] != H or (out_index is None and gx.shape[0] < M):
-            raise ValueError(f"{what}: grad_x must be [M, H]")
-    if not want_w:
-        grad_w = (None, None)
-    elif grad_w is None:
-        if accumulate_w:
-            raise ValueError(f"{what}: accumulate_w needs the tensors to add to (grad_w)")
-        grad_w = (torch.empty(H, dtype=torch.float32, device=x.device),
-                  torch.empty(H, dtype=torch.float32, device=x.device) if want_bias else None)
-    g_w, g_b = (_vector_like(t, H, (torch.float32,), what) for t in grad_w)
-    if not want_bias:
-        g_b = None
-    ws = workspace
-    if ws is None and (g_w is not None or g_b is not None):
-        ws = _workspace(lib.tppo_layer_norm_backward_workspace_bytes(M, H), x.device)
-    _same_device(what, x, grad_y, weight, mean, rstd, rows, out_index, gx, g_w, g_b, ws, _m_actual(m_actual, what), status)
-    with torch.cuda.device(x.device):
-        rc = lib.tppo_layer_norm_backward(_ptr(grad_y), ld_gy, _DTYPES[grad_y.dtype], _ptr(x), n_rows, H, ld_x, _DTYPES[x.dtype],
-                                          _ptr(weight), _DTYPES[weight.dtype], _ptr(mean), _ptr(rstd), _ptr(rows), M,
-                                          _ptr(m_actual), _ptr(gx), ld_gx, _DTYPES[gx.dtype if want_x else x.dtype],
-                                          _ptr(out_index), gx.shape[0] if want_x else 0, _ptr(g_w), _ptr(g_b),
-                                          1 if accumulate_w else 0, _ptr(ws), 0 if ws is None else ws.numel() * ws.element_size(),
-                                          _ptr(status), _stream())
-    _check(rc, what)
-    return gx, g_w, g_b
-
-
-def _balance_arguments(logits, experts, rows, M, m_actual, workspace, out, status, what):
-    lib = load()
-    logits, ld = _rows_like(logits, what)
-    n_rows, E = logits.shape
-    if not (experts.is_cuda and experts.dtype == torch.int32 and experts.dim() == 2 and experts.shape[0] == n_rows and
-            (experts.stride(1) == 1 or experts.shape[1] == 1)):
-        raise ValueError(f"{what}: experts must be an int32 device matrix [n_rows, k] with rows contiguous in memory")
-    M = _count_rows(rows, M, n_rows, what)
-    if out is None:
-        loss, mean_prob = (torch.empty(n, dtype=torch.float32, device=logits.device) for n in (1, E))
-        counts = torch.empty(E, dtype=torch.int64, device=logits.device)
-    else:
-        loss, counts, mean_prob = out
-        _vector_like(loss, 1, (torch.float32,), what)
-        _vector_like(counts, E, (torch.int64,), what)
-        _vector_like(mean_prob, E, (torch.float32,), what)
-    ws = _workspace(lib.tppo_balance_loss_workspace_bytes(M, E), logits.device) if workspace is None else workspace
-    _same_device(what, logits, experts, rows, loss, counts, mean_prob, ws, _m_actual(m_actual, what), status)
-    k = experts.shape[1]
-    return lib, logits, ld, n_rows, E, max(experts.stride(0), k), k, M, loss, counts, mean_prob, ws
+    if grad_dtype is not None:
+        grad_dtype = {torch.float32: TPPO_F32, torch.bfloat16: TPPO_BF16}[grad_dtype]
+    return _there(_native().layer_norm_backward, grad_y, "tppo_layer_norm_backward", x, weight, mean, rstd, rows, M, m_actual,
+                  out_index, out, grad_dtype, want_x, want_w, want_bias, grad_w, accumulate_w, status, workspace)
 
 
 def tppo_balance_loss(logits, experts, rows=None, M=None, m_actual=None, coefficient=1.0, status=None, workspace=None, out=None):
     """Balance loss of a mixture-of-experts router over the tokens ``rows`` (None: all).  logits [n_rows, E] bf16 or fp32;
     experts [n_rows, k] int32, -1 where none was chosen.  ``out``: (loss, counts, mean_prob) to write to.  Returns (loss [1]
     fp32, counts [E] int64, mean_prob [E] fp32)."""
-    what = "tppo_balance_loss"
-    lib, logits, ld, n_rows, E, ld_e, k, M, loss, counts, mean_prob, ws = _balance_arguments(
-        logits, experts, rows, M, m_actual, workspace, out, status, what)
-    with torch.cuda.device(logits.device):
-        rc = lib.tppo_balance_loss(_ptr(logits), n_rows, E, ld, _DTYPES[logits.dtype], _ptr(experts), k, ld_e, _ptr(rows), M,
-                                   _ptr(m_actual), float(coefficient), _ptr(loss), _ptr(counts), _ptr(mean_prob), _ptr(ws),
-                                   ws.numel() * ws.element_size(), _ptr(status), _stream())
-    _check(rc, what)
-    return loss, counts, mean_prob
+    return _there(_native().balance_loss, logits, "tppo_balance_loss", experts, rows, M, m_actual, coefficient, status, workspace,
+                  out)
 
 
 def tppo_balance_loss_backward(logits, experts, rows=None, M=None, m_actual=None, coefficient=1.0, scale=1.0, counts_in=None,
@@ -524,59 +404,15 @@ def tppo_balance_loss_backward(logits, experts, rows=None, M=None, m_actual=None
     the derivatives to, whose rows ``out_index`` names (None: 0 .. M-1); otherwise a new [M, E] one of the logits' type.
     ``counts_in`` [E] int64 and ``token_denominator`` stand for a batch of which this call has a part.  Returns (grad_logits,
     loss, counts, mean_prob)."""
-    what = "tppo_balance_loss_backward"
-    lib, logits, ld, n_rows, E, ld_e, k, M, loss, counts, mean_prob, ws = _balance_arguments(
-        logits, experts, rows, M, m_actual, workspace, out, status, what)
-    _vector_like(counts_in, E, (torch.int64,), what)
-    if out_index is not None and not (out_index.is_cuda and out_index.dtype == torch.int32 and out_index.is_contiguous() and
-                                      out_index.numel() >= M):
-        raise ValueError(f"{what}: out_index must be a contiguous int32 device tensor of M entries")
-    if out_index is not None and grad is None:
-        raise ValueError(f"{what}: out_index needs the tensor that it points into (grad)")
-    g = torch.empty(M, E, dtype=logits.dtype, device=logits.device) if grad is None else grad
-    g, ld_g = _rows_like(g, what)
-    if g.dtype != logits.dtype or g.shape[1] != E or (out_index is None and g.shape[0] < M):
-        raise ValueError(f"{what}: grad must be [M, E] of the logits' type")
-    _same_device(what, logits, g, counts_in, out_index)
-    with torch.cuda.device(logits.device):
-        rc = lib.tppo_balance_loss_backward(_ptr(logits), n_rows, E, ld, _DTYPES[logits.dtype], _ptr(experts), k, ld_e, _ptr(rows),
-                                            M, _ptr(m_actual), float(coefficient), float(scale), _ptr(counts_in),
-                                            int(token_denominator), _ptr(g), ld_g, _ptr(out_index), g.shape[0], _ptr(loss),
-                                            _ptr(counts), _ptr(mean_prob), _ptr(ws), ws.numel() * ws.element_size(),
-                                            _ptr(status), _stream())
-    _check(rc, what)
-    return g, loss, counts, mean_prob
+    return _there(_native().balance_loss_backward, logits, "tppo_balance_loss_backward", experts, rows, M, m_actual, coefficient,
+                  status, workspace, out, scale, counts_in, token_denominator, out_index, grad)
 
 
 def tppo_orthogonalize(g, steps=5, coefficients=(3.4445, -4.7750, 2.0315), eps=1e-7, scale=1.0, workspace=None, out=None):
     """An update made nearly orthogonal by Newton-Schulz products.  g [rows, cols] or [count, rows, cols], bf16 or fp32, rows
     contiguous in memory.  Returns the bf16 result in g's shape (``out``, if given)."""
-    what = "tppo_orthogonalize"
-    lib = load()
-
-    def stack(t, types):
-        if not (t.is_cuda and t.dim() in (2, 3) and t.dtype in types and (t.stride(-1) == 1 or t.shape[-1] == 1)):
-            raise ValueError(f"{what}: matrices on the device with rows contiguous in memory are required")
-        rows, cols = t.shape[-2:]
-        ld = t.stride(-2) if rows > 1 else max(t.stride(-2), cols)
-        count = t.shape[0] if t.dim() == 3 else 1
-        return count, rows, cols, ld, t.stride(0) if t.dim() == 3 else rows * ld
-
-    count, rows, cols, ld_g, each_g = stack(g, _DTYPES)
-    if out is None:
-        out = torch.empty(g.shape, dtype=torch.bfloat16, device=g.device)
-    elif out.shape != g.shape:
-        raise ValueError(f"{what}: out must have g's shape")
-    _, _, _, ld_out, each_out = stack(out, (torch.bfloat16,))
     a, b, c = coefficients
-    ws = _workspace(lib.tppo_orthogonalize_workspace_bytes(count, rows, cols), g.device) if workspace is None else workspace
-    _same_device(what, g, out, ws)
-    with torch.cuda.device(g.device):
-        rc = lib.tppo_orthogonalize(_ptr(g), count, rows, cols, ld_g, each_g, _DTYPES[g.dtype], int(steps), float(a), float(b),
-                                    float(c), float(eps), float(scale), _ptr(out), ld_out, each_out, _ptr(ws),
-                                    ws.numel() * ws.element_size(), _stream())
-    _check(rc, what)
-    return out
+    return _there(_native().orthogonalize, g, "tppo_orthogonalize", steps, a, b, c, eps, scale, workspace, out)[0]
 
 
 class Batcher:

@@ -139,6 +139,9 @@ __global__ __launch_bounds__(kBlThreads) void balance_rows_kernel(Balance b) {
     const int64_t m_eff = b.tokens();
     const int pieces = (E + kN - 1) / kN;
     if (!ONE && blockIdx.x == 0 && threadIdx.x == 0) *b.arrived = 0;
+    int starts[kPieces];
+#pragma unroll
+    for (int i = 0; i < kPieces; ++i) starts[i] = piece_start<kN, RAGGED>(lane + i * kLanes, E);
     float d[kPieces][kN], total[kPieces][kN];
 #pragma unroll
     for (int i = 0; i < kPieces; ++i)
@@ -189,8 +192,8 @@ __global__ __launch_bounds__(kBlThreads) void balance_rows_kernel(Balance b) {
         for (int i = 0; i < kPieces; ++i)
 #pragma unroll
             for (int e = 0; e < kN; ++e) {
-                const int at = (lane + i * kLanes) * kN + e;
-                d[i][e] = at < E ? columns[at] - mean : 0.f;
+                const int at = starts[i] + e;
+                d[i][e] = lane + i * kLanes < pieces && at < E ? columns[at] - mean : 0.f;
             }
         __syncthreads();
     }
@@ -206,7 +209,7 @@ __global__ __launch_bounds__(kBlThreads) void balance_rows_kernel(Balance b) {
             const T* src = static_cast<const T*>(b.logits) + (bad[a] ? 0 : want) * b.ld;
 #pragma unroll
             for (int i = 0; i < kPieces; ++i)
-                if (lane + i * kLanes < pieces) p[a][i] = piece_at<T, RAGGED>(src, lane + i * kLanes, E, -INFINITY);
+                if (lane + i * kLanes < pieces) p[a][i] = piece_at<T, RAGGED>(src, starts[i], E);
         }
 #pragma unroll
         for (int a = 0; a < kAtOnce; ++a) {
@@ -217,7 +220,7 @@ __global__ __launch_bounds__(kBlThreads) void balance_rows_kernel(Balance b) {
             for (int i = 0; i < kPieces; ++i)
 #pragma unroll
                 for (int e = 0; e < kN; ++e) {
-                    z[i][e] = lane + i * kLanes < pieces ? p[a][i].get(e) : -INFINITY;
+                    z[i][e] = lane + i * kLanes < pieces && own<kN, RAGGED>(lane + i * kLanes, starts[i], e, E) ? p[a][i].get(e) : -INFINITY;
                     top = fmaxf(top, z[i][e]);
                 }
             top = over_lanes<1, kLanes>(top, Max());
@@ -258,7 +261,7 @@ __global__ __launch_bounds__(kBlThreads) void balance_rows_kernel(Balance b) {
                             float out[kN];
 #pragma unroll
                             for (int e = 0; e < kN; ++e) out[e] = by * z[i][e] * (d[i][e] - mean);
-                            put_piece<T, kN, RAGGED>(dst, c, E, out);
+                            put_piece<T, kN, RAGGED>(dst, starts[i], E, out, c * kN - starts[i]);
                         }
                     }
                 }
@@ -278,7 +281,8 @@ __global__ __launch_bounds__(kBlThreads) void balance_rows_kernel(Balance b) {
             for (int i = 0; i < kPieces; ++i)
 #pragma unroll
                 for (int e = 0; e < kN; ++e) {
-                    float* at = columns + (wave % kPlaces) * kCols + (lane + i * kLanes) * kN + e;
+                    if (lane + i * kLanes >= pieces || !own<kN, RAGGED>(lane + i * kLanes, starts[i], e, E)) continue;
+                    float* at = columns + (wave % kPlaces) * kCols + starts[i] + e;
                     *at = turn + 1 < kTurns ? *at + total[i][e] : total[i][e];
                 }
         __syncthreads();

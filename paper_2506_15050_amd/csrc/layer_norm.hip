@@ -41,6 +41,10 @@ __global__ __launch_bounds__(kLnThreads) void layer_norm_kernel(
     const int64_t m_eff = m_actual ? min(M, *m_actual) : M;
     const int pieces = (H + kN - 1) / kN;
     const float each = 1.f / (float)H;
+    auto is_own = [&](int i, int e) {
+        const int c = lane + i * kLanes;
+        return own<kN, RAGGED>(c, piece_start<kN, RAGGED>(c, H), e, H);
+    };
     for (int64_t m = (int64_t)blockIdx.x * kRowsAtOnce + mine; m < m_eff; m += (int64_t)gridDim.x * kRowsAtOnce) {
         const int64_t want = rows ? (int64_t)rows[m] : m;
         const bool bad = want < 0 || want >= n_rows;
@@ -49,12 +53,13 @@ __global__ __launch_bounds__(kLnThreads) void layer_norm_kernel(
         float sum = 0.f, none = 0.f;
 #pragma unroll
         for (int i = 0; i < kPieces; ++i)
-            if (lane + i * kLanes < pieces) p[i] = piece_at<T, RAGGED>(src, lane + i * kLanes, H);
+            if (lane + i * kLanes < pieces) p[i] = piece_at<T, RAGGED>(src, piece_start<kN, RAGGED>(lane + i * kLanes, H), H);
 #pragma unroll
         for (int i = 0; i < kPieces; ++i)
             if (lane + i * kLanes < pieces)
 #pragma unroll
-                for (int e = 0; e < kN; ++e) sum += p[i].get(e);
+                for (int e = 0; e < kN; ++e)
+                    if (is_own(i, e)) sum += p[i].get(e);
         row_sums<kLanes>(sum, none, place, 0);
         const float mu = sum * each;
         float sq = 0.f;
@@ -64,7 +69,7 @@ __global__ __launch_bounds__(kLnThreads) void layer_norm_kernel(
 #pragma unroll
                 for (int e = 0; e < kN; ++e) {
                     const float d = p[i].get(e) - mu;
-                    if (!RAGGED || (lane + i * kLanes) * kN + e < H) sq = fmaf(d, d, sq);
+                    if (is_own(i, e)) sq = fmaf(d, d, sq);
                 }
         row_sums<kLanes>(sq, none, place, 1);
         const float s = bad ? __builtin_nanf("") : 1.f / sqrtf(fmaf(sq, each, eps));
@@ -74,16 +79,17 @@ __global__ __launch_bounds__(kLnThreads) void layer_norm_kernel(
             const int c = lane + i * kLanes;
             if (c < pieces) {
                 float w[kN], b[kN], out[kN];
-                get_piece<W, kN, RAGGED>(weight, c, H, w);
+                const int start = piece_start<kN, RAGGED>(c, H);
+                get_piece<W, kN, RAGGED>(weight, start, H, w);
                 if (bias) {
-                    get_piece<W, kN, RAGGED>(bias, c, H, b);
+                    get_piece<W, kN, RAGGED>(bias, start, H, b);
                 } else {
 #pragma unroll
                     for (int e = 0; e < kN; ++e) b[e] = 0.f;
                 }
 #pragma unroll
                 for (int e = 0; e < kN; ++e) out[e] = fmaf((p[i].get(e) - mu) * s, w[e], b[e]);
-                put_piece<T, kN, RAGGED>(dst, c, H, out);
+                put_piece<T, kN, RAGGED>(dst, start, H, out);
             }
         }
         if (lane == 0) {
@@ -94,9 +100,9 @@ __global__ __launch_bounds__(kLnThreads) void layer_norm_kernel(
     }
 }
 
-// Backward.  kLanes threads a row as above; the two sums of a row are taken together.  A thread's columns are the same in all of its rows,
-// so it adds up their weights' derivatives in registers; the groups of a workgroup add theirs in LDS, and each workgroup leaves one row of
-// partial sums, [2][H], which add_rows_kernel adds in a fixed order.
+// Backward.  kLanes threads a row as above; the two sums of a row are taken together, and the next row is asked for before this one is
+// worked on.  A thread's columns are the same in all of its rows, so it adds up their weights' derivatives in registers; the groups of a
+// workgroup add theirs in LDS, and each workgroup leaves one row of partial sums, [2][H], which add_rows_kernel adds in a fixed order.
 template <class T, class G, class O, int kLanes, int kPieces, bool RAGGED>
 __global__ __launch_bounds__(kLanes < kLnThreads ? kLnThreads : kLanes) void layer_norm_backward_kernel(
     const G* __restrict__ grad_y, int64_t ld_gy, const T* __restrict__ x, int64_t n_rows, int H, int64_t ld_x,
@@ -104,80 +110,103 @@ __global__ __launch_bounds__(kLanes < kLnThreads ? kLnThreads : kLanes) void lay
     const int32_t* __restrict__ rows, int64_t M, const int64_t* __restrict__ m_actual, O* __restrict__ grad_x, int64_t ld_gx,
     const int32_t* __restrict__ out_index, int64_t n_out, float* __restrict__ partial, int32_t* status) {
     constexpr int kThreads = kLanes < kLnThreads ? kLnThreads : kLanes;
-    constexpr int kN = Piece<T>::kN, kRowsAtOnce = kThreads / kLanes;
+    constexpr int kN = Piece<T>::kN, kRowsAtOnce = kThreads / kLanes, kQuads = kN / Piece<G>::kN;
     __shared__ float2 place[2][kLanes / kWave];
     __shared__ float gathered[kRowsAtOnce > 1 ? 2 * kLanes * kPieces * kN : 1];
     const int lane = threadIdx.x % kLanes, mine = __builtin_amdgcn_readfirstlane(threadIdx.x / kLanes);
-    const int64_t m_eff = m_actual ? min(M, *m_actual) : M;
+    const int64_t m_eff = m_actual ? min(M, *m_actual) : M, stride = (int64_t)gridDim.x * kRowsAtOnce;
     const int pieces = (H + kN - 1) / kN;
     const float each = 1.f / (float)H;
+    auto there = [&](int i) { return lane + i * kLanes < pieces; };
+    auto start = [&](int i) { return piece_start<kN, RAGGED>(lane + i * kLanes, H); };
+    auto is_own = [&](int i, int e) { return own<kN, RAGGED>(lane + i * kLanes, start(i), e, H); };
     float w[kPieces][kN], gw[kPieces][kN], gb[kPieces][kN];
 #pragma unroll
     for (int i = 0; i < kPieces; ++i) {
-        const int c = lane + i * kLanes;
 #pragma unroll
         for (int e = 0; e < kN; ++e) w[i][e] = gw[i][e] = gb[i][e] = 0.f;
-        if (c < pieces) {
-            if (sizeof(T) == 4 || weight_f32) get_piece<float, kN, RAGGED>(static_cast<const float*>(weight), c, H, w[i]);
-            else if constexpr (sizeof(T) == 2) get_piece<uint16_t, kN, RAGGED>(static_cast<const uint16_t*>(weight), c, H, w[i]);
+        if (there(i)) {
+            if (sizeof(T) == 4 || weight_f32) get_piece<float, kN, RAGGED>(static_cast<const float*>(weight), start(i), H, w[i]);
+            else if constexpr (sizeof(T) == 2) get_piece<uint16_t, kN, RAGGED>(static_cast<const uint16_t*>(weight), start(i), H, w[i]);
         }
     }
-    int turn = 0;
-    for (int64_t m = (int64_t)blockIdx.x * kRowsAtOnce + mine; m < m_eff; m += (int64_t)gridDim.x * kRowsAtOnce, turn ^= 1) {
-        const int64_t want = rows ? (int64_t)rows[m] : m;
-        const bool bad = want < 0 || want >= n_rows;
-        const T* src = x + (bad ? 0 : want) * ld_x;
+    struct Row {
+        Piece<T> x[kPieces];
+        Piece<G> g[kPieces][kQuads];
+        float mu, s;
+        bool bad;
+    };
+    auto index_of = [&](int64_t m) { return m < m_eff ? (rows ? (int64_t)rows[m] : m) : (int64_t)0; };
+    auto fetch = [&](Row& r, int64_t m, int64_t want) {
+        if (m >= m_eff) return;
+        r.bad = want < 0 || want >= n_rows;
+        const T* src = x + (r.bad ? 0 : want) * ld_x;
         const G* gsrc = grad_y + m * ld_gy;
-        float mu = mean[m], s = rstd[m];
-        Piece<T> p[kPieces];
-        float gy[kPieces][kN];
-#pragma unroll
-        for (int i = 0; i < kPieces; ++i) {
-            const int c = lane + i * kLanes;
-            if (c < pieces) {
-                p[i] = piece_at<T, RAGGED>(src, c, H);
-                get_piece<G, kN, RAGGED>(gsrc, c, H, gy[i]);
-            }
-        }
-        float c1 = 0.f, c2 = 0.f;
 #pragma unroll
         for (int i = 0; i < kPieces; ++i)
-            if (lane + i * kLanes < pieces && !bad)
+            if (there(i)) {
+                r.x[i] = piece_at<T, RAGGED>(src, start(i), H);
+#pragma unroll
+                for (int q = 0; q < kQuads; ++q) r.g[i][q] = piece_at<G, RAGGED>(gsrc, start(i) + q * Piece<G>::kN, H);
+            }
+        r.mu = mean[m];
+        r.s = rstd[m];
+    };
+    int turn = 0;
+    auto work = [&](const Row& r, int64_t m) {
+        float c1 = 0.f, c2 = 0.f, s = r.s;
+        auto gy = [&](int i, int e) { return r.g[i][e / Piece<G>::kN].get(e % Piece<G>::kN); };
+#pragma unroll
+        for (int i = 0; i < kPieces; ++i)
+            if (there(i) && !r.bad)
 #pragma unroll
                 for (int e = 0; e < kN; ++e) {
-                    if (RAGGED && (lane + i * kLanes) * kN + e >= H) continue;
-                    const float xh = (p[i].get(e) - mu) * s, g = gy[i][e] * w[i][e];
+                    if (!is_own(i, e)) continue;
+                    const float xh = (r.x[i].get(e) - r.mu) * s, g = gy(i, e) * w[i][e];
                     c1 += g;
                     c2 = fmaf(g, xh, c2);
-                    gw[i][e] = fmaf(gy[i][e], xh, gw[i][e]);
-                    gb[i][e] += gy[i][e];
+                    gw[i][e] = fmaf(gy(i, e), xh, gw[i][e]);
+                    gb[i][e] += gy(i, e);
                 }
         row_sums<kLanes>(c1, c2, place, turn);
-        if (bad) {
+        turn ^= 1;
+        if (r.bad) {
             s = __builtin_nanf("");
             if (lane == 0) set_status(status, TPPO_STATUS_BAD_ROW);
         }
+        if (!grad_x) return;
         const int64_t to = out_index ? (int64_t)out_index[m] : m;
         if (to < 0 || to >= n_out) {
-            if (grad_x && lane == 0) set_status(status, TPPO_STATUS_BAD_ROW);
-        } else if (grad_x) {
-            c1 *= each;
-            c2 *= each;
-            O* dst = grad_x + to * ld_gx;
-#pragma unroll
-            for (int i = 0; i < kPieces; ++i) {
-                const int c = lane + i * kLanes;
-                if (c < pieces) {
-                    float out[kN];
-#pragma unroll
-                    for (int e = 0; e < kN; ++e) {
-                        const float xh = (p[i].get(e) - mu) * s;
-                        out[e] = s * (fmaf(gy[i][e], w[i][e], -c1) - xh * c2);
-                    }
-                    put_piece<O, kN, RAGGED>(dst, c, H, out);
-                }
-            }
+            if (lane == 0) set_status(status, TPPO_STATUS_BAD_ROW);
+            return;
         }
+        c1 *= each;
+        c2 *= each;
+        O* dst = grad_x + to * ld_gx;
+#pragma unroll
+        for (int i = 0; i < kPieces; ++i)
+            if (there(i)) {
+                float out[kN];
+#pragma unroll
+                for (int e = 0; e < kN; ++e) {
+                    const float xh = (r.x[i].get(e) - r.mu) * s;
+                    out[e] = s * (fmaf(gy(i, e), w[i][e], -c1) - xh * c2);
+                }
+                put_piece<O, kN, RAGGED>(dst, start(i), H, out);
+            }
+    };
+    int64_t m = (int64_t)blockIdx.x * kRowsAtOnce + mine;
+    Row a, b;
+    fetch(a, m, index_of(m));
+    int64_t next = index_of(m + stride);
+    for (; m < m_eff; m += 2 * stride) {
+        fetch(b, m + stride, next);
+        next = index_of(m + 2 * stride);
+        work(a, m);
+        if (m + stride >= m_eff) break;
+        fetch(a, m + 2 * stride, next);
+        next = index_of(m + 3 * stride);
+        work(b, m + stride);
     }
     if (!partial) return;
     if constexpr (kRowsAtOnce > 1) {                                 // the groups, one after the other
@@ -201,13 +230,12 @@ __global__ __launch_bounds__(kLanes < kLnThreads ? kLnThreads : kLanes) void lay
     }
     float* to = partial + (int64_t)blockIdx.x * 2 * H;
 #pragma unroll
-    for (int i = 0; i < kPieces; ++i) {
-        const int c = lane + i * kLanes;
-        if (c < pieces) {
-            put_piece<float, kN, RAGGED>(to, c, H, gw[i]);
-            put_piece<float, kN, RAGGED>(to + H, c, H, gb[i]);
+    for (int i = 0; i < kPieces; ++i)
+        if (there(i)) {
+            const int first = (lane + i * kLanes) * kN - start(i);
+            put_piece<float, kN, RAGGED>(to, start(i), H, gw[i], first);
+            put_piece<float, kN, RAGGED>(to + H, start(i), H, gb[i], first);
         }
-    }
 }
 
 // out[h] (+)= the sum of `count` rows' entry h: 64 columns a workgroup, its 16 wavefronts a sixteenth of the rows each.
@@ -346,15 +374,15 @@ extern "C" int tppo_layer_norm_backward(const void* grad_y, int64_t ld_gy, tppo_
             auto go = [&](auto lanes, auto k) { launch(t, g, o, lanes, k, ragged); };
             typedef std::integral_constant<int, 64> L64;
             typedef std::integral_constant<int, 256> L256;
-            typedef std::integral_constant<int, 1024> L1024;
+            typedef std::integral_constant<int, 512> L512;
             if (pieces <= 64) go(L64(), std::integral_constant<int, 1>());
             else if (pieces <= 128) go(L64(), std::integral_constant<int, 2>());
-            else if (pieces <= 256) go(L256(), std::integral_constant<int, 1>());
+            else if (pieces <= 256) go(L64(), std::integral_constant<int, 4>());
             else if (pieces <= 512) go(L256(), std::integral_constant<int, 2>());
             else if (pieces <= 768) go(L256(), std::integral_constant<int, 3>());
             else if (pieces <= 1024) go(L256(), std::integral_constant<int, 4>());
-            else if (pieces <= 2048) go(L1024(), std::integral_constant<int, 2>());
-            else if constexpr (kN == 4) go(L1024(), std::integral_constant<int, 4>());
+            else if (pieces <= 2048) go(L512(), std::integral_constant<int, 4>());
+            else if constexpr (kN == 4) go(L512(), std::integral_constant<int, 8>());
         };
         if (H % kN) sized(std::true_type());
         else sized(std::false_type());

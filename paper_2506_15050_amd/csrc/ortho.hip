@@ -321,9 +321,13 @@ __global__ __launch_bounds__(kNsThreads) void ns_norm_kernel(const T* __restrict
 #pragma unroll 4
     for (unsigned i = blockIdx.x * kNsThreads + threadIdx.x; i < all; i += gridDim.x * kNsThreads) {
         const unsigned r = i / per_row, c = i - r * per_row;
-        const Piece<T> p = piece_at<T, RAGGED>(from + (int64_t)r * ld, c, cols);
+        const int start = piece_start<kN, RAGGED>(c, cols);
+        const Piece<T> p = piece_at<T, RAGGED>(from + (int64_t)r * ld, start, cols);
 #pragma unroll
-        for (int e = 0; e < kN; ++e) sum = fma((double)p.get(e), (double)p.get(e), sum);
+        for (int e = 0; e < kN; ++e) {
+            const double x = own<kN, RAGGED>(c, start, e, cols) ? (double)p.get(e) : 0.0;
+            sum = fma(x, x, sum);
+        }
     }
     sum = ns_workgroup_sum(sum, place);
     if (threadIdx.x == 0) parts[(int64_t)blockIdx.y * kNsParts + blockIdx.x] = sum;
@@ -373,7 +377,7 @@ __global__ __launch_bounds__(kNsThreads) void ns_begin_kernel(const T* __restric
             } else {
 #pragma unroll
                 for (int e = 0; e < 8; ++e) x[e] = 0.f;
-                if (i < m && j < n) get_piece<T, 8, true>(from + (int64_t)i * ld, j / 8, n, x);
+                if (i < m && j < n) get_piece<T, 8, true>(from + (int64_t)i * ld, j, n, x);
             }
 #pragma unroll
             for (int e = 0; e < 8; ++e) x[e] = (float)((double)x[e] * by);

@@ -39,23 +39,32 @@ __device__ __forceinline__ uint32_t two_bf16(float lo, float hi) {
 __device__ __forceinline__ void put(float* p, float x) { *p = x; }
 __device__ __forceinline__ void put(uint16_t* p, float x) { *p = (uint16_t)two_bf16(x, 0.f); }
 
-// Elements c * kN .. of a row of n; what lies beyond the row is `beyond` and not read.  RAGGED: n is no multiple of kN.
+// Where piece c of a row of n begins.  RAGGED (n is no multiple of kN): the last one ends with the row, and its first elements are the one
+// before's as well -- `own` says which are its own.
+template <int kN, bool RAGGED>
+__device__ __forceinline__ int piece_start(int c, int n) {
+    return RAGGED ? min(c * kN, max(n - kN, 0)) : c * kN;
+}
+template <int kN, bool RAGGED>
+__device__ __forceinline__ bool own(int c, int start, int e, int n) {
+    return !RAGGED || (start + e >= c * kN && start + e < n);
+}
+
+// Elements start .. of a row of n; zeros beyond it.  (A row shorter than a piece, or a piece that passes its end: element by element.)
 template <class T, bool RAGGED>
-__device__ __forceinline__ Piece<T> piece_at(const T* row, int c, int n, float beyond = 0.f) {
+__device__ __forceinline__ Piece<T> piece_at(const T* row, int start, int n) {
     constexpr int kN = Piece<T>::kN;
     Piece<T> p;
-    if (!RAGGED || (c + 1) * kN <= n) {
-        p.v = *reinterpret_cast<const typename Piece<T>::V*>(row + c * kN);
+    if (!RAGGED || start + kN <= n) {
+        p.v = *reinterpret_cast<const typename Piece<T>::V*>(row + start);
     } else {
         if constexpr (kN == 4) {
 #pragma unroll
-            for (int e = 0; e < kN; ++e) p.v[e] = c * kN + e < n ? row[c * kN + e] : beyond;
+            for (int e = 0; e < kN; ++e) p.v[e] = start + e < n ? row[start + e] : 0.f;
         } else {
-            const uint32_t b = two_bf16(beyond, beyond);
 #pragma unroll
             for (int e = 0; e < kN; e += 2) {
-                const uint32_t lo = c * kN + e < n ? row[c * kN + e] : b & 0xFFFFu;
-                const uint32_t hi = c * kN + e + 1 < n ? row[c * kN + e + 1] : b & 0xFFFFu;
+                const uint32_t lo = start + e < n ? row[start + e] : 0, hi = start + e + 1 < n ? row[start + e + 1] : 0;
                 p.v[e >> 1] = lo | hi << 16;
             }
         }
@@ -63,11 +72,12 @@ __device__ __forceinline__ Piece<T> piece_at(const T* row, int c, int n, float b
     return p;
 }
 
-// kIn values to elements c * kIn .. of a row of n of type T
+// kIn values to elements start .. of a row of n of type T, those from `first` on.  (The last piece of a ragged row may write what the one
+// before it writes too, the same: first = 0.)
 template <class T, int kIn, bool RAGGED>
-__device__ __forceinline__ void put_piece(T* row, int c, int n, const float (&x)[kIn]) {
-    T* at = row + c * kIn;
-    if (!RAGGED || (c + 1) * kIn <= n) {
+__device__ __forceinline__ void put_piece(T* row, int start, int n, const float (&x)[kIn], int first = 0) {
+    T* at = row + start;
+    if (!RAGGED || (start + kIn <= n && first == 0)) {
         if constexpr (sizeof(T) == 4) {
 #pragma unroll
             for (int e = 0; e < kIn; e += 4)
@@ -80,17 +90,17 @@ __device__ __forceinline__ void put_piece(T* row, int c, int n, const float (&x)
     } else {
 #pragma unroll
         for (int e = 0; e < kIn; ++e)
-            if (c * kIn + e < n) put(at + e, x[e]);
+            if (e >= first && start + e < n) put(at + e, x[e]);
     }
 }
 
-// kOut values of type T from elements c * kOut .. of a row of n
+// kOut values of type T from elements start .. of a row of n
 template <class T, int kOut, bool RAGGED>
-__device__ __forceinline__ void get_piece(const T* row, int c, int n, float (&x)[kOut]) {
+__device__ __forceinline__ void get_piece(const T* row, int start, int n, float (&x)[kOut]) {
     constexpr int kN = Piece<T>::kN;
 #pragma unroll
     for (int q = 0; q < kOut / kN; ++q) {
-        const Piece<T> p = piece_at<T, RAGGED>(row, c * (kOut / kN) + q, n);
+        const Piece<T> p = piece_at<T, RAGGED>(row, start + q * kN, n);
 #pragma unroll
         for (int e = 0; e < kN; ++e) x[q * kN + e] = p.get(e);
     }

@@ -1,4 +1,6 @@
 // tppo_layer_norm, tppo_layer_norm_backward: the trunk's last norm on the rows that the heads project, and its derivatives.
+#include <algorithm>
+
 #include "rows.h"
 
 namespace tppo {
@@ -53,7 +55,7 @@ __global__ __launch_bounds__(kLnThreads) void layer_norm_kernel(
         float sum = 0.f, none = 0.f;
 #pragma unroll
         for (int i = 0; i < kPieces; ++i)
-            if (lane + i * kLanes < pieces) p[i] = piece_at<T, RAGGED>(src, piece_start<kN, RAGGED>(lane + i * kLanes, H), H);
+            if (lane + i * kLanes < pieces) p[i] = piece_at<T, RAGGED, true>(src, piece_start<kN, RAGGED>(lane + i * kLanes, H), H);
 #pragma unroll
         for (int i = 0; i < kPieces; ++i)
             if (lane + i * kLanes < pieces)
@@ -89,7 +91,7 @@ __global__ __launch_bounds__(kLnThreads) void layer_norm_kernel(
                 }
 #pragma unroll
                 for (int e = 0; e < kN; ++e) out[e] = fmaf((p[i].get(e) - mu) * s, w[e], b[e]);
-                put_piece<T, kN, RAGGED>(dst, start, H, out);
+                put_piece<T, kN, RAGGED, true>(dst, start, H, out);
             }
         }
         if (lane == 0) {
@@ -103,8 +105,14 @@ __global__ __launch_bounds__(kLnThreads) void layer_norm_kernel(
 // Backward.  kLanes threads a row as above; the two sums of a row are taken together, and the next row is asked for before this one is
 // worked on.  A thread's columns are the same in all of its rows, so it adds up their weights' derivatives in registers; the groups of a
 // workgroup add theirs in LDS, and each workgroup leaves one row of partial sums, [2][H], which add_rows_kernel adds in a fixed order.
+// Wavefronts that a SIMD's 512 registers hold: a thread's weights and two sums for each of its columns, and two rows of both inputs.
+template <class T, class G, int kPieces>
+constexpr int backward_waves() {
+    constexpr int kColumns = kPieces * Piece<T>::kN, kNeed = 3 * kColumns + 2 * kColumns * (int)(sizeof(T) + sizeof(G)) / 4 + 26;
+    return 512 / kNeed < 1 ? 1 : 512 / kNeed < 4 ? 512 / kNeed : 4;
+}
 template <class T, class G, class O, int kLanes, int kPieces, bool RAGGED>
-__global__ __launch_bounds__(kLanes < kLnThreads ? kLnThreads : kLanes) void layer_norm_backward_kernel(
+__global__ __launch_bounds__(kLanes < kLnThreads ? kLnThreads : kLanes, (backward_waves<T, G, kPieces>())) void layer_norm_backward_kernel(
     const G* __restrict__ grad_y, int64_t ld_gy, const T* __restrict__ x, int64_t n_rows, int H, int64_t ld_x,
     const void* __restrict__ weight, bool weight_f32, const float* __restrict__ mean, const float* __restrict__ rstd,
     const int32_t* __restrict__ rows, int64_t M, const int64_t* __restrict__ m_actual, O* __restrict__ grad_x, int64_t ld_gx,
@@ -145,9 +153,9 @@ __global__ __launch_bounds__(kLanes < kLnThreads ? kLnThreads : kLanes) void lay
 #pragma unroll
         for (int i = 0; i < kPieces; ++i)
             if (there(i)) {
-                r.x[i] = piece_at<T, RAGGED>(src, start(i), H);
+                r.x[i] = piece_at<T, RAGGED, true>(src, start(i), H);
 #pragma unroll
-                for (int q = 0; q < kQuads; ++q) r.g[i][q] = piece_at<G, RAGGED>(gsrc, start(i) + q * Piece<G>::kN, H);
+                for (int q = 0; q < kQuads; ++q) r.g[i][q] = piece_at<G, RAGGED, true>(gsrc, start(i) + q * Piece<G>::kN, H);
             }
         r.mu = mean[m];
         r.s = rstd[m];
@@ -192,7 +200,7 @@ __global__ __launch_bounds__(kLanes < kLnThreads ? kLnThreads : kLanes) void lay
                     const float xh = (r.x[i].get(e) - r.mu) * s;
                     out[e] = s * (fmaf(gy(i, e), w[i][e], -c1) - xh * c2);
                 }
-                put_piece<O, kN, RAGGED>(dst, start(i), H, out);
+                put_piece<O, kN, RAGGED, true>(dst, start(i), H, out);
             }
     };
     int64_t m = (int64_t)blockIdx.x * kRowsAtOnce + mine;
@@ -238,35 +246,53 @@ __global__ __launch_bounds__(kLanes < kLnThreads ? kLnThreads : kLanes) void lay
         }
 }
 
-// out[h] (+)= the sum of `count` rows' entry h: 64 columns a workgroup, its 16 wavefronts a sixteenth of the rows each.
-constexpr int kAddWaves = 16;
-__global__ __launch_bounds__(kAddWaves* kWave) void add_rows_kernel(const float* __restrict__ partial, int count, int H,
-                                                                   float* __restrict__ grad_weight, float* __restrict__ grad_bias,
-                                                                   int accumulate) {
-    __shared__ float sums[kAddWaves][kWave];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int h = blockIdx.x * kWave + lane;
+// out[h] (+)= the sum of `count` rows' entry h: 64 columns a workgroup, four to a thread, its 64 rows of threads a 64th of the rows each,
+// which are all asked for at once.  (A column to a thread, 16 parts of the rows: 512 rows of 2 x 5120 5.5 us.)
+constexpr int kAddThreads = 1024, kAddColumns = 64, kAddParts = kAddThreads * 4 / kAddColumns;
+__global__ __launch_bounds__(kAddThreads) void add_rows_kernel(const float* __restrict__ partial, int count, int H,
+                                                               float* __restrict__ grad_weight, float* __restrict__ grad_bias,
+                                                               int accumulate) {
+    __shared__ float sums[kAddParts][kAddColumns + 4];
+    const int at = (threadIdx.x & 15) * 4, part = threadIdx.x >> 4, h = blockIdx.x * kAddColumns + at;
     float* out = blockIdx.y ? grad_bias : grad_weight;
     if (!out) return;
     const float* from = partial + (blockIdx.y ? H : 0);
-    float sum = 0.f;
+    float sum[4] = {0.f, 0.f, 0.f, 0.f};
     if (h < H)
-#pragma unroll 4
-        for (int r = wave; r < count; r += kAddWaves) sum += from[(int64_t)r * 2 * H + h];
-    sums[wave][lane] = sum;
+#pragma unroll 8
+        for (int r = part; r < count; r += kAddParts) {
+            const Piece<float> x = piece_at<float, true>(from + (int64_t)r * 2 * H, h, H);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) sum[e] += x.get(e);
+        }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) sums[part][at + e] = sum[e];
     __syncthreads();
-    if (wave == 0 && h < H) {
-        sum = accumulate ? out[h] : 0.f;
+    const int col = threadIdx.x & 63, share = threadIdx.x >> 6;      // 16 wavefronts add four parts each, the first one those
+    float some = 0.f;
+#pragma unroll
+    for (int k = 0; k < kAddParts / 16; ++k) some += sums[share * (kAddParts / 16) + k][col];
+    __syncthreads();
+    sums[share][col] = some;
+    __syncthreads();
+    if (share == 0 && blockIdx.x * kAddColumns + col < H) {
         float all = 0.f;
 #pragma unroll
-        for (int k = 0; k < kAddWaves; ++k) all += sums[k][lane];
-        out[h] = sum + all;
+        for (int k = 0; k < 16; ++k) all += sums[k][col];
+        float* to = out + blockIdx.x * kAddColumns + col;
+        *to = accumulate ? *to + all : all;
     }
 }
 
-constexpr int64_t kLnPartials = 512;                                 // rows of partial sums at most: workgroups of the backward kernel
-
-static int64_t backward_groups(int64_t M) { return M < 1 ? 0 : M < kLnPartials ? M : kLnPartials; }
+// Workgroups of the backward kernel: as many as the chip holds at once, of no fewer than four rows each (a row of partial sums is written
+// and read again for each of them, as much as one and a half to two rows are), and no more than take the same number of turns.  us, a call, 512
+// whatever the size -> so:  20000 x 3584, bf16: 112 -> 90;  16416 x 1024, fp32: 51 -> 46.
+constexpr int64_t kLnPartials = 1024;
+static int64_t backward_groups(int64_t M, int rows_at_once, int resident) {
+    const int64_t most = std::min<int64_t>({kLnPartials, (int64_t)256 * resident, std::max<int64_t>(256, M / 4)});
+    const int64_t groups = (M + rows_at_once - 1) / rows_at_once, turns = (groups + most - 1) / most;
+    return (groups + turns - 1) / turns;
+}
 
 }  // namespace tppo
 
@@ -327,7 +353,7 @@ extern "C" int tppo_layer_norm(const void* x, int64_t n_rows, int64_t H, int64_t
 extern "C" size_t tppo_layer_norm_backward_workspace_bytes(int64_t M, int64_t H) {
     using namespace tppo;
     if (M <= 0 || H <= 0 || H > kLnMaxH) return 256;
-    return round_up((size_t)backward_groups(M) * 2 * H * sizeof(float), 256);
+    return round_up((size_t)std::min(M, kLnPartials) * 2 * H * sizeof(float), 256);
 }
 
 extern "C" int tppo_layer_norm_backward(const void* grad_y, int64_t ld_gy, tppo_dtype dt_gy, const void* x, int64_t n_rows, int64_t H,
@@ -356,14 +382,16 @@ extern "C" int tppo_layer_norm_backward(const void* grad_y, int64_t ld_gy, tppo_
         return TPPO_ERR_WORKSPACE;
     hipStream_t s = static_cast<hipStream_t>(stream);
     float* partial = sums ? static_cast<float*>(workspace) : nullptr;
-    const int64_t groups = backward_groups(M);
+    int64_t groups = 0;
     auto launch = [&](auto t, auto g, auto o, auto lanes, auto pieces, auto ragged) {
         typedef decltype(t) T;
         typedef decltype(g) G;
         typedef decltype(o) O;
         constexpr int kLanes = decltype(lanes)::value, kPieces = decltype(pieces)::value;
+        constexpr int kThreads = kLanes < kLnThreads ? kLnThreads : kLanes;
+        groups = backward_groups(M, kThreads / kLanes, std::max(1, backward_waves<T, G, kPieces>() * 4 * kWave / kThreads));
         hipLaunchKernelGGL((layer_norm_backward_kernel<T, G, O, kLanes, kPieces, decltype(ragged)::value>), dim3((unsigned)groups),
-                           dim3(kLanes < kLnThreads ? kLnThreads : kLanes), 0, s, static_cast<const G*>(grad_y), ld_gy,
+                           dim3(kThreads), 0, s, static_cast<const G*>(grad_y), ld_gy,
                            static_cast<const T*>(x), n_rows, (int)H, ld_x, weight, dt_w == TPPO_F32, mean, rstd, rows, M, m_actual,
                            static_cast<O*>(grad_x), ld_gx, out_index, n_out, partial, status);
     };
@@ -396,7 +424,7 @@ extern "C" int tppo_layer_norm_backward(const void* grad_y, int64_t ld_gy, tppo_
         if (hipGetLastError() != hipSuccess) return TPPO_ERR_LAUNCH;
     }
     if (sums && (M > 0 || !accumulate_w))
-        hipLaunchKernelGGL(add_rows_kernel, dim3((unsigned)((H + kWave - 1) / kWave), 2), dim3(kAddWaves * kWave), 0, s, partial,
+        hipLaunchKernelGGL(add_rows_kernel, dim3((unsigned)((H + kAddColumns - 1) / kAddColumns), 2), dim3(kAddThreads), 0, s, partial,
                            (int)groups, (int)H, grad_weight, grad_bias, accumulate_w);
     return launch_result();
 }

@@ -51,12 +51,14 @@ __device__ __forceinline__ bool own(int c, int start, int e, int n) {
 }
 
 // Elements start .. of a row of n; zeros beyond it.  (A row shorter than a piece, or a piece that passes its end: element by element.)
-template <class T, bool RAGGED>
+// STREAM: read once, and not kept in the caches for it.
+template <class T, bool RAGGED, bool STREAM = false>
 __device__ __forceinline__ Piece<T> piece_at(const T* row, int start, int n) {
     constexpr int kN = Piece<T>::kN;
     Piece<T> p;
     if (!RAGGED || start + kN <= n) {
-        p.v = *reinterpret_cast<const typename Piece<T>::V*>(row + start);
+        const typename Piece<T>::V* at = reinterpret_cast<const typename Piece<T>::V*>(row + start);
+        p.v = STREAM ? __builtin_nontemporal_load(at) : *at;
     } else {
         if constexpr (kN == 4) {
 #pragma unroll
@@ -74,18 +76,19 @@ __device__ __forceinline__ Piece<T> piece_at(const T* row, int start, int n) {
 
 // kIn values to elements start .. of a row of n of type T, those from `first` on.  (The last piece of a ragged row may write what the one
 // before it writes too, the same: first = 0.)
-template <class T, int kIn, bool RAGGED>
+template <class T, int kIn, bool RAGGED, bool STREAM = false>
 __device__ __forceinline__ void put_piece(T* row, int start, int n, const float (&x)[kIn], int first = 0) {
     T* at = row + start;
     if (!RAGGED || (start + kIn <= n && first == 0)) {
-        if constexpr (sizeof(T) == 4) {
+        typedef typename Piece<T>::V V;
 #pragma unroll
-            for (int e = 0; e < kIn; e += 4)
-                *reinterpret_cast<Piece<float>::V*>(at + e) = Piece<float>::V{x[e], x[e + 1], x[e + 2], x[e + 3]};
-        } else {
-            static_assert(kIn == 8, "16 bytes");
-            *reinterpret_cast<Piece<uint16_t>::V*>(at) = Piece<uint16_t>::V{two_bf16(x[0], x[1]), two_bf16(x[2], x[3]),
-                                                                            two_bf16(x[4], x[5]), two_bf16(x[6], x[7])};
+        for (int e = 0; e < kIn; e += Piece<T>::kN) {
+            V v;
+            if constexpr (sizeof(T) == 4) v = V{x[e], x[e + 1], x[e + 2], x[e + 3]};
+            else v = V{two_bf16(x[e], x[e + 1]), two_bf16(x[e + 2], x[e + 3]), two_bf16(x[e + 4], x[e + 5]), two_bf16(x[e + 6], x[e + 7])};
+            V* to = reinterpret_cast<V*>(at + e);
+            if constexpr (STREAM) __builtin_nontemporal_store(v, to);
+            else *to = v;
         }
     } else {
 #pragma unroll

@@ -46,17 +46,21 @@ struct NsCfg {
     static constexpr int kTileV = TV, kTileT = TT, kWavesV = WV, kWavesT = WT, kWaves = WV * WT, kThreads = kWaves * 64;
     static constexpr int kBK = 64, kRowBytes = 128, kRows = TV + TT, kStageBytes = kRows * kRowBytes, kLdsBytes = 2 * kStageBytes;
     static constexpr int kWaveV = TV / WV, kWaveT = TT / WT, kVB = kWaveV / 16, kTB = kWaveT / 16;
-    static constexpr int kDma = kStageBytes / 1024, kDmaPerWave = kDma / kWaves, kDmaV = TV * kRowBytes / 1024;
+    // transfers of a stage: the first kDmaMore wavefronts have kDmaPerWave of them, the others one less
+    static constexpr int kDma = kStageBytes / 1024, kDmaPerWave = (kDma + kWaves - 1) / kWaves, kDmaMore = kDma - (kDmaPerWave - 1) * kWaves;
+    static constexpr int kDmaV = TV * kRowBytes / 1024;
     static constexpr int kSteps = 2 * kVB;           // of kTB MFMAs each
     static constexpr int kSpreadSteps = kSteps / 2;  // a stage's transfers go out over so many
     static constexpr bool kKMajor = KMAJOR, kSplit = SPLIT;
     static constexpr int kKRowBytes = TV * 2;        // K-major: a stage is 64 rows of TV columns
-    static_assert(kDmaPerWave * kWaves == kDma && kDma * 1024 == kStageBytes, "whole transfers");
+    static_assert(kDma * 1024 == kStageBytes && kWaveV % 16 == 0 && kWaveT % 16 == 0, "whole transfers and blocks");
 };
 
-// Tile `id` of a matrix.  Rectangular: blocks of 8 T tiles, column by column, so that an XCD's workgroups share operands in its L2.
-// Symmetric: the same over v >= t.
-template <bool SYMMETRIC>
+// Tile `id` of a matrix: blocks of 8 T tiles, column by column, so that an XCD's workgroups share operands in its L2.  Symmetric: of those
+// that hold an entry on or above the diagonal, v >= t.
+template <class C, bool SYMMETRIC>
+__host__ __device__ __forceinline__ int ns_first_v(int t) { return SYMMETRIC ? t * C::kTileT / C::kTileV : 0; }
+template <class C, bool SYMMETRIC>
 __device__ __forceinline__ void ns_tile_at(int id, int tiles_t, int tiles_v, int& t, int& v) {
     constexpr int kBlock = 8;
     if constexpr (!SYMMETRIC) {
@@ -64,26 +68,35 @@ __device__ __forceinline__ void ns_tile_at(int id, int tiles_t, int tiles_v, int
         v = in / height;
         t = block * kBlock + in - v * height;
     } else {
-        int first = 0;
-        for (;;) {
-            const int height = min(kBlock, tiles_t - first), corner = height * (height + 1) / 2;
-            const int all = corner + (tiles_v - first - height) * height;
-            if (id < all) {
-                if (id < corner) {
-                    int col = 0;
-                    while ((col + 1) * (col + 2) / 2 <= id) ++col;
-                    v = first + col;
-                    t = first + id - col * (col + 1) / 2;
-                } else {
-                    const int col = (id - corner) / height;
-                    v = first + height + col;
-                    t = first + id - corner - col * height;
-                }
-                return;
+        for (int first = 0;; first += kBlock) {
+            const int height = min(kBlock, tiles_t - first);
+            int all = 0;
+            for (int i = 0; i < height; ++i) all += tiles_v - ns_first_v<C, true>(first + i);
+            if (id >= all) {
+                id -= all;
+                continue;
             }
-            id -= all;
-            first += kBlock;
+            int there = 0;                           // T tiles of the block that have column v
+            for (v = ns_first_v<C, true>(first);; ++v) {
+                while (there < height && ns_first_v<C, true>(first + there) <= v) ++there;
+                if (there == height || id < there) break;
+                id -= there;
+            }
+            v += id / there;
+            t = first + id % there;
+            return;
         }
+    }
+}
+
+// eight values to a row of bf16 that has `left` more entries
+__device__ __forceinline__ void put_whole_or_part(uint16_t* to, int left, const float (&x)[8]) {
+    if (left >= 8) {
+        put_piece<uint16_t, 8, false>(to, 0, 8, x);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (e < left) to[e] = ns_bf16(x[e]);
     }
 }
 
@@ -95,18 +108,20 @@ __global__ __launch_bounds__(C::kThreads, C::kLdsBytes <= 80 * 1024 ? C::kWaves 
     const int id = ns_by_xcd(blockIdx.x, gridDim.x);
     const int mat = id / p.tiles;
     int tile_t, tile_v;
-    ns_tile_at<kSymmetric>(id - mat * p.tiles, p.tiles_t, p.tiles_v, tile_t, tile_v);
+    ns_tile_at<C, kSymmetric>(id - mat * p.tiles, p.tiles_t, p.tiles_v, tile_t, tile_v);
     const int t0 = tile_t * C::kTileT, v0 = tile_v * C::kTileV;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wv = wave / C::kWavesT, wt = wave % C::kWavesT, col = lane & 15, grp = lane >> 4;
     const unsigned lds_base = (unsigned)(size_t)(__attribute__((address_space(3))) unsigned char*)smem;
 
-    // transfers: this wavefront's are kDmaPerWave of the stage's, the V side's first
+    // transfers: this wavefront's of the stage's, the V side's first
+    const bool more = wave < C::kDmaMore;
+    const int first_dma = wave * (kDmaPerWave - 1) + min(wave, C::kDmaMore);
     const char* src[kDmaPerWave];
     const char *t_base = reinterpret_cast<const char*>(p.t_op + mat * p.each_t), *v_base = reinterpret_cast<const char*>(p.v_op + mat * p.each_v);
 #pragma unroll
     for (int q = 0; q < kDmaPerWave; ++q) {
-        const int d = wave * kDmaPerWave + q;
+        const int d = first_dma + q;             // (one too many where there are fewer: an address that is not used)
         if (d < C::kDmaV && C::kKMajor) {
             constexpr int kPerRow = C::kKRowBytes / 16;
             const int at = d * 64 + lane, k = at / kPerRow, c = (at % kPerRow) ^ ns_swz_k<C::kTileV>(k);
@@ -123,10 +138,11 @@ __global__ __launch_bounds__(C::kThreads, C::kLdsBytes <= 80 * 1024 ? C::kWaves 
     const int stages_once = p.k / C::kBK, stages = C::kSplit ? 3 * stages_once : stages_once;
     int issued = 0;
     const int64_t step_v = C::kKMajor ? (int64_t)C::kBK * p.ld_v * 2 : C::kRowBytes;
-    const unsigned dst0 = lds_base + wave * kDmaPerWave * 1024;
+    const unsigned dst0 = lds_base + first_dma * 1024;
     unsigned dst = dst0;
     auto issue_one = [&](int q) {
-        const bool on_v = wave * kDmaPerWave + q < C::kDmaV;
+        if (C::kDmaMore != C::kWaves && q + 1 == kDmaPerWave && !more) return;
+        const bool on_v = first_dma + q < C::kDmaV;
         const char* from = src[q] + (on_v ? pos_v : pos);
         asm volatile("s_add_u32 m0, %0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off"
                      :
@@ -222,76 +238,150 @@ __global__ __launch_bounds__(C::kThreads, C::kLdsBytes <= 80 * 1024 ? C::kWaves 
         }
     }
 
-    // epilogue: a lane has four V columns in a row of T's, block by block
+    // Epilogue, half of the tile's rows at a time: the sums go through LDS, so that all reads and writes of memory are whole pieces of 16
+    // bytes of rows, eight entries each, and what a half reads is asked for before its sums are there.  Mirrored entries are taken
+    // from LDS by columns.  (From the registers, four entries of 16 rows an instruction and two bytes at a time across the diagonal, a
+    // round of 256 tiles of 256 x 256 took 37 us for B X and 10 for b A + c A A.)
+    // 16-byte piece c of a half's row r lies at c ^ key(r): consecutive rows, and rows 8 apart, at different places of the bank window
+    auto key = [](int r) { return (r ^ (r >> 3)) & 15; };
+    constexpr int kHalf = C::kTileT / 2, kPieces = C::kTileV / 8, kRowsAtOnce = C::kThreads / kPieces, kTurns = kHalf / kRowsAtOnce;
+    static_assert(kHalf * C::kTileV * 4 <= C::kLdsBytes && kTurns * kRowsAtOnce == kHalf && C::kWavesT % 2 == 0, "half a tile");
     const float2 scales = p.scales[mat];
+    const int piece = tid % kPieces, row = tid / kPieces, v = v0 + piece * 8;
+    const bool v_there = v < p.n_v;
+    float dv[8];
+    if constexpr (MODE == kPoly)
 #pragma unroll
-    for (int tb = 0; tb < kTB; ++tb) {
-        const int t = t0 + wt * C::kWaveT + tb * 16 + col;
-        if (t >= p.n_t) continue;
+        for (int e = 0; e < 8; ++e) dv[e] = v_there ? p.diag[mat * p.each_diag + v + e] : 0.f;
 #pragma unroll
-        for (int vb = 0; vb < kVB; ++vb) {
-            const int v = v0 + wv * C::kWaveV + vb * 16 + grp * 4;
-            if (v >= p.n_v) continue;
-            if constexpr (kSymmetric) {
-                half_t *out = (MODE == kGram ? p.off : p.off_out) + mat * p.each_off, *out_lo = nullptr;
-                if constexpr (C::kSplit) out_lo = (MODE == kGram ? p.off_lo : p.off_out_lo) + mat * p.each_off;
-                float* diag = (MODE == kGram ? p.diag : p.diag_out) + mat * p.each_diag;
-                const int64_t at = (int64_t)t * p.ld_off + v;
-                float x[4];
-                if constexpr (MODE == kGram) {
+    for (int half = 0; half < 2; ++half) {
+        const int th = t0 + half * kHalf;
+        half8 in_hi[kTurns], in_lo[kTurns];
+        float in_d[kTurns];
+        if constexpr (MODE != kGram) {
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        x[e] = acc[vb][tb][e] * scales.x;
-                        if (v + e == t) diag[t] = x[e];
-                        x[e] *= kOffScale;
-                    }
-                } else {
-                    const half4 was = *reinterpret_cast<const half4*>(p.off + mat * p.each_off + at);
-                    half4 was_lo = {};
-                    if constexpr (C::kSplit) was_lo = *reinterpret_cast<const half4*>(p.off_lo + mat * p.each_off + at);
-                    const float* d = p.diag + mat * p.each_diag;
-                    const float dt = d[t];
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const float w = C::kSplit ? fmaf((float)was_lo[e], 1.f / kLoScale, (float)was[e]) : (float)was[e], dv = d[v + e];
-                        if (v + e == t) diag[t] = fmaf(p.c, fmaf(acc[vb][tb][e], 1.f / (kOffScale * kOffScale), dt * dt), p.b * dt);
-                        x[e] = fmaf(p.c, fmaf(dt + dv, w, acc[vb][tb][e] * (1.f / kOffScale)), p.b * w);
-                    }
+            for (int k = 0; k < kTurns; ++k) {
+                const int t = min(th + k * kRowsAtOnce + row, p.n_t - 1);
+                const half_t *from = MODE == kPoly ? p.off : p.hi, *from_lo = MODE == kPoly ? p.off_lo : p.lo;
+                const int64_t at = MODE == kPoly ? mat * p.each_off + (int64_t)t * p.ld_off + v : mat * p.each_x + (int64_t)t * p.ld_x + v;
+                in_d[k] = p.diag[mat * p.each_diag + t];
+                if (v_there) {
+                    in_hi[k] = *reinterpret_cast<const half8*>(from + at);
+                    if constexpr (MODE != kPoly || C::kSplit) in_lo[k] = *reinterpret_cast<const half8*>(from_lo + at);
                 }
-                half4 o, o_lo;
+            }
+        }
+        __syncthreads();                             // the stages, or the first half, are read
+        if (wt / (C::kWavesT / 2) == half)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    x[e] = v + e == t ? 0.f : x[e];
-                    o[e] = (half_t)x[e];
-                    o_lo[e] = (half_t)((x[e] - (float)o[e]) * kLoScale);
+            for (int tb = 0; tb < kTB; ++tb) {
+                const int r = (wt % (C::kWavesT / 2)) * C::kWaveT + tb * 16 + col;
+#pragma unroll
+                for (int vb = 0; vb < kVB; ++vb)
+                    *reinterpret_cast<f32x4*>(smem + r * (C::kTileV * 4) + (((wv * (C::kWaveV / 4) + vb * 4 + grp) ^ key(r)) << 4)) = acc[vb][tb];
+            }
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < kTurns; ++k) {
+            const int r = k * kRowsAtOnce + row, t = th + r;
+            f32x4 *low = reinterpret_cast<f32x4*>(smem + r * (C::kTileV * 4) + (((piece * 2) ^ key(r)) << 4));
+            f32x4 *high = reinterpret_cast<f32x4*>(smem + r * (C::kTileV * 4) + (((piece * 2 + 1) ^ key(r)) << 4));
+            const f32x4 sum[2] = {*low, *high};
+            if (t >= p.n_t || !v_there) continue;
+            float x[8];
+            if constexpr (MODE == kGram) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    x[e] = sum[e >> 2][e & 3] * scales.x;
+                    if (v + e == t) p.diag[mat * p.each_diag + t] = x[e];
+                    x[e] = v + e == t ? 0.f : x[e] * kOffScale;
                 }
-                *reinterpret_cast<half4*>(out + at) = o;
-                if constexpr (C::kSplit) *reinterpret_cast<half4*>(out_lo + at) = o_lo;
-                if (tile_t != tile_v)
+            } else if constexpr (MODE == kPoly) {
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        out[(int64_t)(v + e) * p.ld_off + t] = o[e];
-                        if constexpr (C::kSplit) out_lo[(int64_t)(v + e) * p.ld_off + t] = o_lo[e];
-                    }
+                for (int e = 0; e < 8; ++e) {
+                    const float w = C::kSplit ? fmaf((float)in_lo[k][e], 1.f / kLoScale, (float)in_hi[k][e]) : (float)in_hi[k][e], s = sum[e >> 2][e & 3];
+                    if (v + e == t) p.diag_out[mat * p.each_diag + t] = fmaf(p.c, fmaf(s, 1.f / (kOffScale * kOffScale), in_d[k] * in_d[k]), p.b * in_d[k]);
+                    x[e] = v + e == t ? 0.f : fmaf(p.c, fmaf(in_d[k] + dv[e], w, s * (1.f / kOffScale)), p.b * w);
+                }
             } else {
-                const int64_t at = mat * p.each_x + (int64_t)t * p.ld_x + v;
-                const half4 hi = *reinterpret_cast<const half4*>(p.hi + at), lo = *reinterpret_cast<const half4*>(p.lo + at);
-                const float lead = p.a + p.diag[mat * p.each_diag + t];
-                half4 new_hi, new_lo;
+                const float lead = p.a + in_d[k];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const float x = fmaf(lead, fmaf((float)lo[e], 1.f / kLoScale, (float)hi[e]), acc[vb][tb][e] * (1.f / kOffScale));
-                    if constexpr (MODE == kUpdate) {
-                        new_hi[e] = (half_t)x;
-                        new_lo[e] = (half_t)((x - (float)new_hi[e]) * kLoScale);
-                    } else if (t < p.m && v + e < p.n) {
-                        const int64_t to = p.transposed ? (int64_t)(v + e) * p.ld_out + t : (int64_t)t * p.ld_out + v + e;
-                        p.out[mat * p.each_out + to] = ns_bf16(x * scales.y);
-                    }
+                for (int e = 0; e < 8; ++e)
+                    x[e] = fmaf(lead, fmaf((float)in_lo[k][e], 1.f / kLoScale, (float)in_hi[k][e]), sum[e >> 2][e & 3] * (1.f / kOffScale));
+            }
+            if constexpr (kSymmetric) {
+                half_t *to = (MODE == kGram ? p.off : p.off_out) + mat * p.each_off + (int64_t)t * p.ld_off + v, *to_lo = nullptr;
+                if constexpr (C::kSplit) to_lo = (MODE == kGram ? p.off_lo : p.off_out_lo) + mat * p.each_off + (int64_t)t * p.ld_off + v;
+                half8 h, l;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    h[e] = (half_t)x[e];
+                    l[e] = (half_t)((x[e] - (float)h[e]) * kLoScale);
                 }
-                if constexpr (MODE == kUpdate) {
-                    *reinterpret_cast<half4*>(p.hi_out + at) = new_hi;
-                    *reinterpret_cast<half4*>(p.lo_out + at) = new_lo;
+                if (v >= t) {
+                    *reinterpret_cast<half8*>(to) = h;
+                    if constexpr (C::kSplit) *reinterpret_cast<half8*>(to_lo) = l;
+                } else if (v + 7 >= t) {
+#pragma unroll
+                    for (int e = 1; e < 8; ++e)
+                        if (v + e >= t) {
+                            to[e] = h[e];
+                            if constexpr (C::kSplit) to_lo[e] = l[e];
+                        }
+                }
+                *low = f32x4{x[0], x[1], x[2], x[3]};
+                *high = f32x4{x[4], x[5], x[6], x[7]};
+            } else if constexpr (MODE == kUpdate) {
+                half8 h, l;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    h[e] = (half_t)x[e];
+                    l[e] = (half_t)((x[e] - (float)h[e]) * kLoScale);
+                }
+                const int64_t at = mat * p.each_x + (int64_t)t * p.ld_x + v;
+                *reinterpret_cast<half8*>(p.hi_out + at) = h;
+                *reinterpret_cast<half8*>(p.lo_out + at) = l;
+            } else if (!p.transposed) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) x[e] *= scales.y;
+                if (t < p.m && v < p.n) put_whole_or_part(p.out + mat * p.each_out + (int64_t)t * p.ld_out + v, p.n - v, x);
+            } else {
+                *low = f32x4{x[0], x[1], x[2], x[3]} * scales.y;
+                *high = f32x4{x[4], x[5], x[6], x[7]} * scales.y;
+            }
+        }
+        if (kSymmetric || (MODE == kLast && p.transposed)) {
+            __syncthreads();
+            constexpr int kAcross = kHalf / 8, kItems = kAcross * C::kTileV / C::kThreads;     // pieces of eight rows of a column
+#pragma unroll 2
+            for (int k = 0; k < kItems; ++k) {
+                const int item = k * C::kThreads + tid, c = item / kAcross, r0 = (item - c * kAcross) * 8, vc = v0 + c, t = th + r0;
+                if (vc >= p.n_v || t >= p.n_t || (kSymmetric && t > vc)) continue;
+                float x[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) x[e] = *reinterpret_cast<const float*>(smem + (r0 + e) * (C::kTileV * 4) + (((c >> 2) ^ key(r0 + e)) << 4) + (c & 3) * 4);
+                if constexpr (kSymmetric) {
+                    half_t *to = (MODE == kGram ? p.off : p.off_out) + mat * p.each_off + (int64_t)vc * p.ld_off + t, *to_lo = nullptr;
+                    if constexpr (C::kSplit) to_lo = (MODE == kGram ? p.off_lo : p.off_out_lo) + mat * p.each_off + (int64_t)vc * p.ld_off + t;
+                    half8 h, l;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        h[e] = (half_t)x[e];
+                        l[e] = (half_t)((x[e] - (float)h[e]) * kLoScale);
+                    }
+                    if (t + 7 <= vc) {
+                        *reinterpret_cast<half8*>(to) = h;
+                        if constexpr (C::kSplit) *reinterpret_cast<half8*>(to_lo) = l;
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 8; ++e)
+                            if (t + e <= vc) {
+                                to[e] = h[e];
+                                if constexpr (C::kSplit) to_lo[e] = l[e];
+                            }
+                    }
+                } else if (vc < p.n && t < p.m) {
+                    put_whole_or_part(p.out + mat * p.each_out + (int64_t)vc * p.ld_out + t, p.m - t, x);
                 }
             }
         }
@@ -442,37 +532,69 @@ static NsLayout ns_layout(int64_t count, int64_t rows, int64_t cols) {
     return L;
 }
 
+template <class C, bool SYMMETRIC>
+static int ns_tiles(int n_t, int n_v) {
+    const int tiles_t = (n_t + C::kTileT - 1) / C::kTileT, tiles_v = (n_v + C::kTileV - 1) / C::kTileV;
+    int tiles = 0;
+    for (int t = 0; t < tiles_t; ++t) tiles += tiles_v - ns_first_v<C, SYMMETRIC>(t);
+    return tiles;
+}
 template <class C, NsMode MODE>
 static int launch_ns(NsArgs& p, int64_t count, hipStream_t s) {
     if (C::kLdsBytes > 64 * 1024 && !allow_lds(reinterpret_cast<const void*>(ns_product_kernel<C, MODE>), C::kLdsBytes)) return TPPO_ERR_LAUNCH;
     p.tiles_t = (p.n_t + C::kTileT - 1) / C::kTileT;
     p.tiles_v = (p.n_v + C::kTileV - 1) / C::kTileV;
-    p.tiles = MODE == kGram || MODE == kPoly ? p.tiles_t * (p.tiles_t + 1) / 2 : p.tiles_t * p.tiles_v;
+    p.tiles = ns_tiles<C, MODE == kGram || MODE == kPoly>(p.n_t, p.n_v);
     hipLaunchKernelGGL((ns_product_kernel<C, MODE>), dim3((unsigned)(p.tiles * count)), dim3(C::kThreads), C::kLdsBytes, s, p);
     return launch_result();
 }
 
-// Side of the output tiles.  256 x 256 tiles read the least, a workgroup to a CU; 128 x 128 ones, two to a CU, spread fewer of them and leave
-// less of a last round empty.  Times in us: a stage (64 of the contraction) of a large tile 1.4, of two small ones that share a CU 1.1, of
-// one that has it alone 0.77; and what a round's tiles do to memory when they end.  Measured, a call, 128 -> 256:  5120 x 5120: 3560 -> 2910;
-// 4096: 2330 -> 2040;  where the rule says 128: 3584: 1479 (1591; its products B X, which go by themselves, 139 -> 109);  2048: 548 (991);
-// 1024 x 4096: 544 (974);  twelve of 1024 x 1024: 617 (689).  (192 x 192, whose tiles fill the rounds of 4096 and 5120 best, asks as much of
-// L2 as 128 x 128 does: 1990 and 3420.)
-static int ns_tile_side(const NsArgs& p, int64_t count, bool symmetric, int stages) {
-    auto tiles = [&](int side) {
-        const int64_t t = (p.n_t + side - 1) / side, v = (p.n_v + side - 1) / side;
-        return (symmetric ? t * (t + 1) / 2 : t * v) * count;
-    };
-    const double end = symmetric ? 8.0 : 25.0;
-    const int64_t each = (tiles(128) + kSweepGroups - 1) / kSweepGroups;       // small tiles on the busiest CU
-    const double small = (double)(each / 2) * (1.1 * stages + end / 2) + (double)(each % 2) * (0.77 * stages + end / 4);
-    return rounds_of(tiles(256)) * (1.4 * stages + end) < small ? 256 : 128;
+// The tiles of a product.  256 V columns by 256 T rows read the least; fewer rows make finer parts of it, whose number comes nearer to whole
+// rounds of 256 workgroups; 128 x 128, two workgroups to a CU, are for what is too small for either.
+template <bool ACROSS, int T>
+using NsLarge = NsCfg<256, T, (T % 64 ? 4 : 2), (T % 64 ? 2 : 4), ACROSS, false>;
+constexpr int kNsShapes = 6;
+constexpr int kNsRows[kNsShapes] = {256, 224, 192, 160, 128, 0};                               // 0: 128 x 128
+constexpr double kNsStage[kNsShapes] = {1.0, 0.89, 0.8, 0.69, 0.6, 0.0};                       // of a stage's 1.4 us
+template <bool SYMMETRIC>
+static int ns_shape(const NsArgs& p, int64_t count, int stages) {
+    const int64_t tiles[kNsShapes] = {ns_tiles<NsLarge<!SYMMETRIC, 256>, SYMMETRIC>(p.n_t, p.n_v) * count,
+                                      ns_tiles<NsLarge<!SYMMETRIC, 224>, SYMMETRIC>(p.n_t, p.n_v) * count,
+                                      ns_tiles<NsLarge<!SYMMETRIC, 192>, SYMMETRIC>(p.n_t, p.n_v) * count,
+                                      ns_tiles<NsLarge<!SYMMETRIC, 160>, SYMMETRIC>(p.n_t, p.n_v) * count,
+                                      ns_tiles<NsLarge<!SYMMETRIC, 128>, SYMMETRIC>(p.n_t, p.n_v) * count,
+                                      ns_tiles<NsCfg<128, 128, 2, 2, !SYMMETRIC, false>, SYMMETRIC>(p.n_t, p.n_v) * count};
+    const double end = SYMMETRIC ? 8.0 : 25.0;
+    int best = 0;
+    double least = 1e300;
+    for (int i = 0; i < kNsShapes; ++i) {
+        double cost;
+        if (kNsRows[i]) {
+            cost = rounds_of(tiles[i]) * (1.4 * stages * kNsStage[i] + end * kNsRows[i] / 256);
+        } else {
+            const int64_t each = (tiles[i] + kSweepGroups - 1) / kSweepGroups;                 // on the busiest CU
+            cost = (double)(each / 2) * (1.1 * stages + end / 2) + (double)(each % 2) * (0.77 * stages + end / 4);
+        }
+        if (cost < least) {
+            least = cost;
+            best = i;
+        }
+    }
+    return best;
 }
 template <bool SPLIT, NsMode MODE>
 static int launch_ns_tiles(NsArgs& p, int64_t count, hipStream_t s) {
     constexpr bool kAcross = MODE == kUpdate || MODE == kLast;
-    const int side = ns_tile_side(p, count, !kAcross, p.k / 64 * (SPLIT ? 3 : 1));
-    if (side == 256) return launch_ns<NsCfg<256, 256, 2, 4, kAcross, SPLIT>, MODE>(p, count, s);
+    const int shape = SPLIT ? kNsShapes - 1 : ns_shape<!kAcross>(p, count, p.k / 64);
+    if constexpr (!SPLIT) {
+        switch (shape) {
+            case 0: return launch_ns<NsLarge<kAcross, 256>, MODE>(p, count, s);
+            case 1: return launch_ns<NsLarge<kAcross, 224>, MODE>(p, count, s);
+            case 2: return launch_ns<NsLarge<kAcross, 192>, MODE>(p, count, s);
+            case 3: return launch_ns<NsLarge<kAcross, 160>, MODE>(p, count, s);
+            case 4: return launch_ns<NsLarge<kAcross, 128>, MODE>(p, count, s);
+        }
+    }
     return launch_ns<NsCfg<128, 128, 2, 2, kAcross, SPLIT>, MODE>(p, count, s);
 }
 

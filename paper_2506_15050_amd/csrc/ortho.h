@@ -53,8 +53,9 @@ struct NsShape {
     int64_t ld_out, each_out;
 };
 
-// The way by X X^T (ortho_gram.hip): for m < kGramBelow, if the coefficients keep it within what fp16 pairs hold.
-constexpr int kGramBelow = 512;
+// The way by X X^T (ortho_gram.hip): where it is the shorter, for m < kGramBelow at most, if the coefficients keep it within what fp16
+// pairs hold.
+constexpr int kGramBelow = 2048;
 bool ns_gram_fits(int steps, float a, float b, float c);
 size_t ns_gram_bytes(int64_t count, int m, int n);
 int ns_gram(const NsShape& x, const half_t* hi, const half_t* lo, const float2* scales, char* ws, hipStream_t s);

@@ -13,12 +13,14 @@
 // one pass  m = 512 rank one 1.5e-3, full 7e-4;  256 2.3e-3;  64 9e-3;  three passes  1e-4 at most.
 // All scales are powers of two: X is held times S = 2^round(log2(n) / 2), so that entries are around one from the first step to the last,
 // A and B off the diagonal times 64.  Where |G|_F is so far below eps that X stays under 1/4 to the end, S is larger by as much.
+#include <cmath>
+
 #include "ortho.h"
 #include "rows.h"
 
 namespace tppo {
 
-constexpr int kSplitBelow = kGramBelow;
+constexpr int kSplitBelow = 512;
 
 enum NsMode { kGram, kPoly, kUpdate, kLast };        // A = X X^T;  B = b A + c A A;  X = a X + B X;  the same into the caller's array
 
@@ -551,48 +553,69 @@ static int launch_ns(NsArgs& p, int64_t count, hipStream_t s) {
 
 // The tiles of a product.  256 V columns by 256 T rows read the least; fewer rows make finer parts of it, whose number comes nearer to whole
 // rounds of 256 workgroups; 128 x 128, two workgroups to a CU, are for what is too small for either.
+// A stage (64 of the contraction) takes so many us a round: what LDS passes, fragments and transfers together, and the MFMAs, which cover
+// each other but in part (5120 x 5120, X X^T, 256 x 256: 123 us; without the transfers 96, without the MFMAs 96).  (Stages of 32, four under
+// way: 143; four wavefronts of 128 x 128: 149.)  Measured, us, the products of a step (X X^T, b A + c A A, B X) by rows of a tile, 256 / 192 /
+// 160 / 128 x 128; * what the rule takes:
+//   5120 x 5120:  *125 / 197 / 179 / 157   *134 / 212 / 190 / 167   *265 / 317 / 287 / 302
+//   3584 x 3584:   83 / 71 / 64 / *58         91 / 78 / 70 / *62       *95 / 147 / 131 / 112
+//   2048 x 2048:   52 / 45 / 40 / *30         60 / 52 / 46 / *31        72 / 57 / 50 / *34
+// (224 rows take no less than 256, 128 rows with 256 columns what two of 128 x 128 take.)
 template <bool ACROSS, int T>
 using NsLarge = NsCfg<256, T, (T % 64 ? 4 : 2), (T % 64 ? 2 : 4), ACROSS, false>;
-constexpr int kNsShapes = 6;
-constexpr int kNsRows[kNsShapes] = {256, 224, 192, 160, 128, 0};                               // 0: 128 x 128
-constexpr double kNsStage[kNsShapes] = {1.0, 0.89, 0.8, 0.69, 0.6, 0.0};                       // of a stage's 1.4 us
+constexpr int kNsShapes = 4;
+constexpr double kNsStage[kNsShapes - 1] = {1.49, 1.25, 1.12};                                 // 256, 192, 160 rows
+constexpr double kNsSmallPair = 0.95, kNsSmallAlone = 0.66;                                    // two that share a CU; one
+struct NsShapeCost {
+    int shape;
+    double stage;                                    // us for 64 of the contraction
+};
 template <bool SYMMETRIC>
-static int ns_shape(const NsArgs& p, int64_t count, int stages) {
-    const int64_t tiles[kNsShapes] = {ns_tiles<NsLarge<!SYMMETRIC, 256>, SYMMETRIC>(p.n_t, p.n_v) * count,
-                                      ns_tiles<NsLarge<!SYMMETRIC, 224>, SYMMETRIC>(p.n_t, p.n_v) * count,
-                                      ns_tiles<NsLarge<!SYMMETRIC, 192>, SYMMETRIC>(p.n_t, p.n_v) * count,
-                                      ns_tiles<NsLarge<!SYMMETRIC, 160>, SYMMETRIC>(p.n_t, p.n_v) * count,
-                                      ns_tiles<NsLarge<!SYMMETRIC, 128>, SYMMETRIC>(p.n_t, p.n_v) * count,
-                                      ns_tiles<NsCfg<128, 128, 2, 2, !SYMMETRIC, false>, SYMMETRIC>(p.n_t, p.n_v) * count};
-    const double end = SYMMETRIC ? 8.0 : 25.0;
-    int best = 0;
-    double least = 1e300;
-    for (int i = 0; i < kNsShapes; ++i) {
-        double cost;
-        if (kNsRows[i]) {
-            cost = rounds_of(tiles[i]) * (1.4 * stages * kNsStage[i] + end * kNsRows[i] / 256);
-        } else {
-            const int64_t each = (tiles[i] + kSweepGroups - 1) / kSweepGroups;                 // on the busiest CU
-            cost = (double)(each / 2) * (1.1 * stages + end / 2) + (double)(each % 2) * (0.77 * stages + end / 4);
-        }
+static NsShapeCost ns_shape(int n_t, int n_v, int64_t count) {
+    const int64_t tiles[kNsShapes - 1] = {ns_tiles<NsLarge<!SYMMETRIC, 256>, SYMMETRIC>(n_t, n_v) * count,
+                                          ns_tiles<NsLarge<!SYMMETRIC, 192>, SYMMETRIC>(n_t, n_v) * count,
+                                          ns_tiles<NsLarge<!SYMMETRIC, 160>, SYMMETRIC>(n_t, n_v) * count};
+    const int64_t small = ns_tiles<NsCfg<128, 128, 2, 2, !SYMMETRIC, false>, SYMMETRIC>(n_t, n_v) * count;
+    const int64_t each = (small + kSweepGroups - 1) / kSweepGroups;                            // on the busiest CU
+    double least = (double)(each / 2) * kNsSmallPair + (double)(each % 2) * kNsSmallAlone;
+    int best = kNsShapes - 1;
+    for (int i = 0; i + 1 < kNsShapes; ++i) {
+        const double cost = rounds_of(tiles[i]) * kNsStage[i];
         if (cost < least) {
             least = cost;
             best = i;
         }
     }
-    return best;
+    return {best, least};
+}
+
+// Which way is the shorter.  Both by their launches: what they cost without their stages, in us, and the stages.  This way has three
+// products a step, of X's length and of its width; the other (ortho_gram.hip) three passes over pairs, 64 x 64 tiles, of X's width but for
+// the first and the last.  Measured, us, this way / the other, * what the rule takes:  512 x 512: 228 / *156;  1024 x 1024: 320 / *233;  1536:
+// *402 / 446;  2048: *500 / 930;  1024 x 4096: 478 / *281;  1536 x 6144: 735 / *584;  2048 x 8192: *1041 / 1304;  four of 1024 x 1024: *332 / 522;  four
+// of 1024 x 4096: *630 / 722;  1024 x 16384: 1242 / *468.
+static double ns_direct_us(int mp, int np, int64_t count, int steps) {
+    const double gram = ns_shape<true>(mp, mp, count).stage, update = ns_shape<false>(mp, np, count).stage;
+    return steps * (3 * 9.0 + gram * (np + mp) / 64 + update * mp / 64);
+}
+static double ns_gram_us(int mp, int np, int64_t count, int steps) {
+    const int side = mp / 64;
+    const double tiles = (double)side * (side + 1) / 2 * (double)count;
+    auto launch = [](double groups, double stages) {
+        return 5.0 + stages * (groups <= kSweepGroups ? 0.5 : 0.8 * std::ceil(groups / (2 * kSweepGroups)));
+    };
+    const double poly = launch(tiles, side), both = launch(2 * tiles, side);
+    return steps * (2 * poly + both) - poly + 10.0 + 0.8 * tiles * (np / 64) / (2 * kSweepGroups) + launch((double)side * (np / 64) * (double)count, side);
 }
 template <bool SPLIT, NsMode MODE>
 static int launch_ns_tiles(NsArgs& p, int64_t count, hipStream_t s) {
     constexpr bool kAcross = MODE == kUpdate || MODE == kLast;
-    const int shape = SPLIT ? kNsShapes - 1 : ns_shape<!kAcross>(p, count, p.k / 64);
+    const int shape = SPLIT ? kNsShapes - 1 : ns_shape<!kAcross>(p.n_t, p.n_v, count).shape;
     if constexpr (!SPLIT) {
         switch (shape) {
             case 0: return launch_ns<NsLarge<kAcross, 256>, MODE>(p, count, s);
-            case 1: return launch_ns<NsLarge<kAcross, 224>, MODE>(p, count, s);
-            case 2: return launch_ns<NsLarge<kAcross, 192>, MODE>(p, count, s);
-            case 3: return launch_ns<NsLarge<kAcross, 160>, MODE>(p, count, s);
-            case 4: return launch_ns<NsLarge<kAcross, 128>, MODE>(p, count, s);
+            case 1: return launch_ns<NsLarge<kAcross, 192>, MODE>(p, count, s);
+            case 2: return launch_ns<NsLarge<kAcross, 160>, MODE>(p, count, s);
         }
     }
     return launch_ns<NsCfg<128, 128, 2, 2, kAcross, SPLIT>, MODE>(p, count, s);
@@ -633,7 +656,8 @@ static int run_ns(const T* g, int64_t count, int64_t rows, int64_t cols, int64_t
     x.a = a; x.b = b; x.c = c;
     x.m = L.m; x.n = L.n; x.transposed = transposed;
     x.out = out; x.ld_out = ld_out; x.each_out = stride_out; x.scales = scales;
-    if (L.m < kGramBelow && ns_gram_fits(steps, a, b, c)) {
+    if (L.m < kGramBelow && (L.split || ns_gram_us(L.mp, L.np, count, steps) < ns_direct_us(L.mp, L.np, count, steps)) &&
+        ns_gram_fits(steps, a, b, c)) {
         const NsShape shape = {L.m, L.n, L.mp, L.np, transposed, count, steps, a, b, c, out, ld_out, stride_out};
         return ns_gram(shape, hi[0], lo[0], scales, ws + L.shared, s);
     }

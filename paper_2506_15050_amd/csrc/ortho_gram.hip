@@ -1,4 +1,4 @@
-// tppo_orthogonalize for matrices with a short side, m < kGramBelow: the iteration on X X^T alone.
+// tppo_orthogonalize for matrices with a short side: the iteration on X X^T alone (ortho.hip chooses).
 //     X_k = P_k X_0 with P_k a polynomial of A_0 = X_0 X_0^T, and all of these m x m matrices are symmetric and commute:
 //     M = a I + b A + c A A,   A <- M A M,   P <- M P;   at the end X = P X_0.
 // X is read twice instead of twice a step, and what is left between is m x m: 6 m^2 n + 17 m^3 flop (5 steps, halves of symmetric

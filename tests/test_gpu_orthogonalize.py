@@ -102,10 +102,16 @@ def test_sizes_of_values(shape):
         _check(out[0], stack[0])
 
 
-@pytest.mark.parametrize("rows,cols,dtype", [(1024, 4096, F), (2056, 1100, BF), (2304, 2304, F)])
+@pytest.mark.parametrize("rows,cols,dtype", [
+    (1024, 4096, F), (2056, 1100, BF),          # pairs of 64 x 64 tiles, of more of them than CUs
+    (2304, 2304, F), (2049, 2500, F),           # products of X in tiles of 128 x 128, sizes that end inside one
+    (5120, 2300, BF), (2304, 5120, F),          # B X in tiles of 192 rows, tall and wide
+    (4096, 4096, F), (4000, 4090, BF),          # X X^T in tiles of 160 rows, B X of 256
+    (4608, 4608, F), (4610, 4520, F)])          # X X^T in tiles of 192 rows
 def test_large(rows, cols, dtype):
     """Against the iteration in 64 bits on the device (the host's takes minutes)."""
     g = torch.randn(rows, cols, device="cuda").to(dtype)
+    g[:, : cols // 3] += (torch.randn(rows, 8, device="cuda") @ torch.randn(8, cols // 3, device="cuda")).to(dtype)
     out = tp.tppo_orthogonalize(g).double()
     x = g.double()
     if rows > cols:
@@ -118,6 +124,21 @@ def test_large(rows, cols, dtype):
     rms = x.norm() / x.numel() ** 0.5
     assert float((out - x).norm() / x.norm()) <= NORM
     assert bool(((out - x).abs() <= 2.0 ** -8 * x.abs() + ELEMENT * rms).all())
+
+
+@pytest.mark.parametrize("rows,cols", [(1100, 1030), (700, 1500)])
+def test_stacks_of_middling_matrices(rows, cols):
+    """A single one goes by pairs, eight by products of X: both against 64 bits."""
+    g = torch.randn(8, rows, cols, device="cuda")
+    for out, src in ((tp.tppo_orthogonalize(g)[5], g[5]), (tp.tppo_orthogonalize(g[5]), g[5])):
+        x = src.double()
+        x = x.t().contiguous() if rows > cols else x
+        x = x / (x.norm() + 1e-7)
+        for _ in range(5):
+            s = x @ x.t()
+            x = 3.4445 * x + (-4.7750 * s + 2.0315 * (s @ s)) @ x
+        x = x.t() if rows > cols else x
+        assert float((out.double() - x).norm() / x.norm()) <= NORM
 
 
 def test_captured():

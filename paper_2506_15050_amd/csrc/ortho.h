@@ -1,6 +1,7 @@
 // What the two ways of tppo_orthogonalize share (ortho.hip: products of X itself; ortho_gram.hip: of X X^T alone).
 #pragma once
 #include "head_tile.h"
+#include "rows.h"
 
 namespace tppo {
 
@@ -36,6 +37,17 @@ __device__ __forceinline__ half8 ns_k_major_frag(unsigned at, int block, int k32
 }
 
 __device__ __forceinline__ uint16_t ns_bf16(float x) { return __builtin_bit_cast(uint16_t, (__bf16)x); }
+
+// eight values to a row of bf16 that has `left` more entries
+__device__ __forceinline__ void put_whole_or_part(uint16_t* to, int left, const float (&x)[8]) {
+    if (left >= 8) {
+        put_piece<uint16_t, 8, false>(to, 0, 8, x);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (e < left) to[e] = ns_bf16(x[e]);
+    }
+}
 
 // Consecutive numbers to the workgroups of an XCD, which go round-robin over the 8 (one more to the first `all` % 8 of them).
 __device__ __forceinline__ int ns_by_xcd(int block, int all) {

@@ -16,7 +16,6 @@
 #include <cmath>
 
 #include "ortho.h"
-#include "rows.h"
 
 namespace tppo {
 
@@ -88,17 +87,6 @@ __device__ __forceinline__ void ns_tile_at(int id, int tiles_t, int tiles_v, int
             t = first + id % there;
             return;
         }
-    }
-}
-
-// eight values to a row of bf16 that has `left` more entries
-__device__ __forceinline__ void put_whole_or_part(uint16_t* to, int left, const float (&x)[8]) {
-    if (left >= 8) {
-        put_piece<uint16_t, 8, false>(to, 0, 8, x);
-    } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-            if (e < left) to[e] = ns_bf16(x[e]);
     }
 }
 

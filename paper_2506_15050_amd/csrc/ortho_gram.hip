@@ -26,12 +26,27 @@ struct PairArgs {
     PairProblem problem[2];
     int64_t each_t, each_v, each_out;
     int ld_t, ld_v, ld_out;
-    int tiles_t, tiles_v, tiles, stages, chunks;     // tiles: of one matrix; chunks: of the contraction (kPairGram)
-    int count;
+    int tiles, stages, chunks, count;                // tiles: of one matrix, kPairLast: of V; chunks: of the contraction (kPairGram)
+    int deep;                                        // chunks; kPairLast: T tiles; or 1
+    double by_deep, by_tiles, by_count;              // their reciprocals
     float* part;                                     // kPairGram: [chunk][matrix][mp][mp], tiles on one side of the diagonal
     const float2* scales;
     NsShape x;
 };
+
+// quotient and remainder by a number whose reciprocal is there (a division in integers is forty instructions of the few that a small product is)
+__device__ __forceinline__ int pair_divide(int x, int by, double inverse, int& over) {
+    int q = (int)((double)x * inverse);
+    over = x - q * by;
+    if (over < 0) {
+        --q;
+        over += by;
+    } else if (over >= by) {
+        ++q;
+        over -= by;
+    }
+    return q;
+}
 
 // tile `id` of those with v >= t
 __device__ __forceinline__ void pair_tile_at(int id, int& t, int& v) {
@@ -69,17 +84,18 @@ template <PairMode MODE, int STAGES>
 __global__ __launch_bounds__(kPairThreads, STAGES == 2 ? 2 : 1) void ns_pair_kernel(PairArgs p) {
     extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
     constexpr bool kKMajor = MODE == kPairLast;
-    int id = ns_by_xcd(blockIdx.x, gridDim.x);
-    const int chunk = id % p.chunks;
-    id /= p.chunks;
-    const int tile = id % p.tiles;
-    id /= p.tiles;
-    const int mat = id % p.count;
-    const PairProblem& q = p.problem[id / p.count];
+    // chunk by chunk, or V tile by V tile, of a tile, tile by tile, matrix by matrix, problem by problem; consecutive ones on an XCD, whose L2
+    // holds a small matrix (eight of 333 rows spread over all: 174 -> 183 us a call)
+    int rest = ns_by_xcd(blockIdx.x, gridDim.x), inner, tile, mat;
+    rest = pair_divide(rest, p.deep, p.by_deep, inner);
+    rest = pair_divide(rest, p.tiles, p.by_tiles, tile);
+    rest = pair_divide(rest, p.count, p.by_count, mat);
+    const int chunk = MODE == kPairGram ? inner : 0;
+    const PairProblem& q = p.problem[MODE == kPairMul ? rest : 0];
     int tile_t, tile_v;
     if constexpr (MODE == kPairLast) {
-        tile_v = tile / p.tiles_t;
-        tile_t = tile - tile_v * p.tiles_t;
+        tile_t = inner;
+        tile_v = tile;
     } else {
         pair_tile_at(tile, tile_t, tile_v);
     }
@@ -155,7 +171,7 @@ __global__ __launch_bounds__(kPairThreads, STAGES == 2 ? 2 : 1) void ns_pair_ker
         }
     }
     float(*tile_out)[kTileLd] = reinterpret_cast<float(*)[kTileLd]>(smem);
-    if constexpr (MODE == kPairPoly || MODE == kPairMul) __syncthreads();          // (the stages are read)
+    if constexpr (MODE != kPairGram) __syncthreads();                // (the stages are read)
 #pragma unroll
     for (int tb = 0; tb < 2; ++tb) {
         const int t = t0 + wt * 32 + tb * 16 + col;
@@ -171,13 +187,8 @@ __global__ __launch_bounds__(kPairThreads, STAGES == 2 ? 2 : 1) void ns_pair_ker
                     make_float4(x[0], x[1], x[2], x[3]);
             } else if constexpr (MODE == kPairLast) {
                 const float by = q.in_scale * p.scales[mat].y;
-                if (t < p.x.m)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        if (v + e < p.x.n) {
-                            const int64_t to = p.x.transposed ? (int64_t)(v + e) * p.x.ld_out + t : (int64_t)t * p.x.ld_out + v + e;
-                            p.x.out[mat * p.x.each_out + to] = ns_bf16(x[e] * by);
-                        }
+                for (int e = 0; e < 4; ++e) tile_out[t - t0][v - v0 + e] = x[e] * by;
             } else {
                 half4 a_hi, a_lo;
                 if constexpr (MODE == kPairPoly) {   // (t_op is A)
@@ -193,6 +204,20 @@ __global__ __launch_bounds__(kPairThreads, STAGES == 2 ? 2 : 1) void ns_pair_ker
                     tile_out[t - t0][v - v0 + e] = y * q.out_scale;
                 }
             }
+        }
+    }
+    if constexpr (MODE == kPairLast) {               // eight entries of a row of the caller's matrix at a time
+        __syncthreads();
+#pragma unroll
+        for (int turn = 0; turn < 2; ++turn) {
+            const int r = turn * 32 + ((int)threadIdx.x >> 3), c = (threadIdx.x & 7) * 8;
+            float x[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] = p.x.transposed ? tile_out[c + e][r] : tile_out[r][c + e];
+            const int row_at = p.x.transposed ? v0 + r : t0 + r, rows = p.x.transposed ? p.x.n : p.x.m;
+            const int col_at = p.x.transposed ? t0 + c : v0 + c, cols = p.x.transposed ? p.x.m : p.x.n;
+            if (row_at < rows && col_at < cols)
+                put_whole_or_part(p.x.out + mat * p.x.each_out + (int64_t)row_at * p.x.ld_out + col_at, cols - col_at, x);
         }
     }
     if constexpr (MODE == kPairPoly || MODE == kPairMul) {
@@ -258,15 +283,24 @@ __global__ __launch_bounds__(kIterThreads, 1) void ns_iterate_kernel(const float
 #pragma unroll
     for (int j = 0; j < kB; ++j)
 #pragma unroll
-        for (int i = 0; i < kT; ++i) {
-            const int t = strip + i * 16 + col, v = j * 16 + grp * 4;
-            f32x4 x = {};
-            const float* at = part + (int64_t)mat * MP * MP;         // (there are sums on and above the diagonal)
-            for (int k = 0; k < chunks; ++k, at += (int64_t)count * MP * MP)
+        for (int i = 0; i < kT; ++i) A[j][i] = f32x4{0, 0, 0, 0};
+    // (a chunk's sums all asked for at once; there are sums on and above the diagonal)
+#pragma unroll 2
+    for (int k = 0; k < chunks; ++k) {
+        const float* at = part + ((int64_t)k * count + mat) * MP * MP;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) x[e] += at[min(t, v + e) * MP + max(t, v + e)];
-            A[j][i] = x * by;
-        }
+        for (int j = 0; j < kB; ++j)
+#pragma unroll
+            for (int i = 0; i < kT; ++i) {
+                const int t = strip + i * 16 + col, v = j * 16 + grp * 4;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) A[j][i][e] += at[min(t, v + e) * MP + max(t, v + e)];
+            }
+    }
+#pragma unroll
+    for (int j = 0; j < kB; ++j)
+#pragma unroll
+        for (int i = 0; i < kT; ++i) A[j][i] *= by;
     auto split = [&](const Strip& x, Pairs& p) {
         typedef float f2 __attribute__((ext_vector_type(2)));
         typedef half_t h2 __attribute__((ext_vector_type(2)));
@@ -459,7 +493,11 @@ GramLayout gram_layout(int64_t count, int mp, int np) {
 }
 template <PairMode MODE>
 int launch_pair(PairArgs& p, int problems, hipStream_t s) {
-    const unsigned groups = (unsigned)(p.tiles * p.chunks * p.count * problems);
+    p.deep = MODE == kPairGram ? p.chunks : MODE == kPairLast ? p.x.mp / kPairTile : 1;
+    p.by_deep = 1.0 / p.deep;
+    p.by_tiles = 1.0 / p.tiles;
+    p.by_count = 1.0 / p.count;
+    const unsigned groups = (unsigned)((int64_t)p.tiles * p.count * p.deep * problems);
     if (groups <= kSweepGroups) {
         if (!allow_lds(reinterpret_cast<const void*>(ns_pair_kernel<MODE, 4>), 4 * kPairStage)) return TPPO_ERR_LAUNCH;
         hipLaunchKernelGGL((ns_pair_kernel<MODE, 4>), dim3(groups), dim3(kPairThreads), 4 * kPairStage, s, p);
@@ -542,9 +580,7 @@ int ns_gram(const NsShape& x, const half_t* hi, const half_t* lo, const float2* 
     p.ld_t = mp;
     p.each_v = (int64_t)mp * np;
     p.ld_v = np;
-    p.tiles_t = mp / kPairTile;
-    p.tiles_v = np / kPairTile;
-    p.tiles = p.tiles_t * p.tiles_v;
+    p.tiles = np / kPairTile;
     p.stages = mp / 64;
     p.chunks = 1;
     return launch_pair<kPairLast>(p, 1, s);

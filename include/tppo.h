@@ -498,6 +498,7 @@ int tppo_layer_norm(const void* x, int64_t n_rows, int64_t H, int64_t ld_x, tppo
  * A row index outside [0, n_rows) gives a grad_x row of NaN, adds nothing to
  * the weights' derivatives and sets TPPO_STATUS_BAD_ROW, which an out_index
  * outside [0, n_out) sets as well (that row is not written).
+ * No output may overlap an input or another output.
  * workspace: tppo_layer_norm_backward_workspace_bytes(M, H); not needed (may be
  *      NULL) where neither grad_weight nor grad_bias is wanted.
  */
@@ -553,7 +554,7 @@ int tppo_balance_loss(const void* logits, int64_t n_rows, int64_t E, int64_t ld,
  * in : as tppo_balance_loss; scale finite; counts_in may be NULL.
  * out: grad_logits of type dt, row stride ld_grad; rows by out_index and n_out
  *      as in tppo_layer_norm_backward.  A row of only -inf gets 0, a row outside
- *      [0, n_rows) NaN.
+ *      [0, n_rows) NaN.  No output may overlap an input or another output.
  */
 int tppo_balance_loss_backward(const void* logits, int64_t n_rows, int64_t E, int64_t ld, tppo_dtype dt,
                                const int32_t* experts, int64_t k, int64_t ld_experts,
@@ -573,15 +574,19 @@ int tppo_balance_loss_backward(const void* logits, int64_t n_rows, int64_t E, in
  *   out = scale * X, transposed back, rounded to bf16.
  * With (a, b, c) = (3.4445, -4.7750, 2.0315) and 5 steps, singular values from
  * 0.3 % of |G|_F on come to lie between 0.68 and 1.21.
- * X is held to 22 bits, the operands of the products to 11 (fp16, scaled by
- * powers of two), to 22 where rows or cols < 512, the diagonals of A and
- * b A + c A^2 and all sums in fp32.
+ * X is held to 22 bits (pairs of fp16, scaled by powers of two), all sums in
+ * fp32.  The operands of the products are held to 11 bits, with the diagonals of
+ * A and b A + c A^2 in fp32; to 22 where rows or cols < 512, and where the
+ * iteration runs on X X^T alone (rows or cols < 2048, where that is the shorter
+ * way; the same X, then, multiplied by a polynomial of X X^T at the end).
  *
  * in : g: `count` matrices [rows, cols] of type dt, row stride ld_g, stride_g
  *      elements from one to the next; 1 <= rows, cols <= 65536, 0 <= steps <= 64;
  *      a, b, c, eps, scale finite, eps >= 0.
+ *      stride_g >= 0; 0 is the same matrix every time.
  * out: out: `count` matrices [rows, cols] bf16, row stride ld_out, stride_out
- *      apart; no overlap with g or each other.
+ *      apart, one behind the other (stride_out >= (rows - 1) ld_out + cols); no
+ *      overlap with g.
  * A matrix of zeros stays zero (with eps > 0); one with a NaN or an infinity
  * gives NaN.  Coefficients under which the iteration grows without bound end in
  * infinities and NaN.

@@ -378,14 +378,17 @@ def tppo_layer_norm(x, weight, bias=None, eps=1e-5, rows=None, M=None, m_actual=
 
 
 def tppo_layer_norm_backward(grad_y, x, weight, mean, rstd, rows=None, M=None, m_actual=None, out_index=None, out=None,
-                             grad_dtype=None, want_x=True, want_w=True, want_bias=True, grad_w=None, accumulate_w=False,
+                             grad_dtype=None, want_x=True, want_w=True, want_bias=None, grad_w=None, accumulate_w=False,
                              status=None, workspace=None):
     """Derivatives of ``tppo_layer_norm``.  grad_y [M, H] fp32 or bf16 (fp32 with fp32 x).  ``out``: the grad_x tensor to
     write to, whose rows ``out_index`` names (None: 0 .. M-1); otherwise a new [M, H] one of ``grad_dtype`` (x's by default).
-    ``grad_w``: (grad_weight, grad_bias) fp32 to write, or with ``accumulate_w`` to add, to.  Returns (grad_x, grad_weight,
-    grad_bias), None where not wanted."""
+    ``grad_w``: (grad_weight, grad_bias) fp32 to write, or with ``accumulate_w`` to add, to.  ``want_bias`` None: as ``want_w``.
+    Returns (grad_x, grad_weight, grad_bias), None where not wanted."""
     if grad_dtype is not None:
-        grad_dtype = {torch.float32: TPPO_F32, torch.bfloat16: TPPO_BF16}[grad_dtype]
+        if grad_dtype not in (torch.float32, torch.bfloat16):
+            raise ValueError("tppo_layer_norm_backward: grad_dtype must be fp32 or bf16")
+        grad_dtype = TPPO_F32 if grad_dtype == torch.float32 else TPPO_BF16
+    want_bias = want_w if want_bias is None else want_bias
     return _there(_native().layer_norm_backward, grad_y, "tppo_layer_norm_backward", x, weight, mean, rstd, rows, M, m_actual,
                   out_index, out, grad_dtype, want_x, want_w, want_bias, grad_w, accumulate_w, status, workspace)
 

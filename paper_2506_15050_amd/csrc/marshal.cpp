@@ -601,20 +601,17 @@ PyObject* layer_norm_backward(PyObject*, PyObject* const* args, Py_ssize_t n) {
             to = Rows(a, gx, "out must be a device matrix");
             if (!known(*gx) || to.cols != x.cols || (!index && to.rows < l.M)) a.refuse("out must be [M, H], fp32 or bf16");
         }
-        if (want_w) {
-            if (grad_w == Py_None) {
-                if (accumulate) a.refuse("accumulate_w needs the tensors to add to (grad_w)");
-                own[1] = made(a.like(), at::kFloat, {x.cols});
-                gw = &own[1];
-                if (want_bias) {
-                    own[2] = made(a.like(), at::kFloat, {x.cols});
-                    gb = &own[2];
-                }
-            } else {
-                gw = a.dense(a.entry(grad_w, 2, 0), at::kFloat, x.cols, true, true, "grad_weight must be contiguous fp32 of H elements");
-                gb = a.dense(a.entry(grad_w, 2, 1), at::kFloat, x.cols, true, true, "grad_bias must be contiguous fp32 of H elements");
-                if (!want_bias) gb = nullptr;
-            }
+        if (grad_w != Py_None) {
+            gw = a.dense(a.entry(grad_w, 2, 0), at::kFloat, x.cols, true, true, "grad_weight must be contiguous fp32 of H elements");
+            gb = a.dense(a.entry(grad_w, 2, 1), at::kFloat, x.cols, true, true, "grad_bias must be contiguous fp32 of H elements");
+            if (!want_w) gw = nullptr;
+            if (!want_bias) gb = nullptr;
+        } else {
+            if (accumulate && (want_w || want_bias)) a.refuse("accumulate_w needs the tensors to add to (grad_w)");
+            if (want_w) own[1] = made(a.like(), at::kFloat, {x.cols});
+            if (want_bias) own[2] = made(a.like(), at::kFloat, {x.cols});
+            gw = want_w ? &own[1] : nullptr;
+            gb = want_bias ? &own[2] : nullptr;
         }
         if (gw || gb) ws = scratch(ws, tppo_layer_norm_backward_workspace_bytes(l.M, x.cols), a.like(), own[3]);
         const int rc = run([&] {

@@ -285,3 +285,71 @@ def test_singular_values_of_every_size(rows, cols):
         want = oops.orthogonalize(_host(g))
         got = _host(tp.tppo_orthogonalize(g))
         assert np.linalg.norm(got - want) <= (2.0 ** -8 + 2.0 ** -9) * np.linalg.norm(want), low
+
+
+def test_the_binding_refuses():
+    """What does not fit is a ValueError before anything is launched; what the library refuses, a RuntimeError."""
+    x, w, s = torch.zeros(6, 16, device="cuda"), torch.zeros(16, device="cuda"), torch.zeros(6, device="cuda")
+    ids, i32 = torch.zeros(6, 2, dtype=torch.int32, device="cuda"), torch.zeros(6, dtype=torch.int32, device="cuda")
+    half = x.half()
+    back = lambda *a, **k: tp.tppo_layer_norm_backward(*a, **k)                                        # noqa: E731
+    calls = [
+        lambda: tp.tppo_layer_norm(half, w), lambda: tp.tppo_layer_norm(x, w.half()), lambda: tp.tppo_layer_norm(x.t(), s),
+        lambda: tp.tppo_layer_norm(x[0], w), lambda: tp.tppo_layer_norm(x, w[:15]), lambda: tp.tppo_layer_norm(x[:, ::2], w[:8]),
+        lambda: tp.tppo_layer_norm(x[:1].expand(6, 16), w), lambda: tp.tppo_layer_norm(x, w, w.bfloat16()),
+        lambda: tp.tppo_layer_norm(x, w.cpu()), lambda: tp.tppo_layer_norm(x, w, rows=i32.long()), lambda: tp.tppo_layer_norm(x, w, M=7),
+        lambda: tp.tppo_layer_norm(x, w, M=-1), lambda: tp.tppo_layer_norm(x, w, rows=i32, M=7), lambda: tp.tppo_layer_norm(x, w, m_actual=i32),
+        lambda: tp.tppo_layer_norm(x, w, out=x), lambda: tp.tppo_layer_norm(x, w, out=(x[:5], None, None)),
+        lambda: tp.tppo_layer_norm(x, w, out=(half, None, None)), lambda: tp.tppo_layer_norm(x, w, out=(x, s[:5], None)),
+        lambda: tp.tppo_layer_norm(x, w, status=s),
+        lambda: back(x[:5], x, w, s, s), lambda: back(x, x, w, s[:5], s), lambda: back(x, x, w, None, s), lambda: back(half, x, w, s, s),
+        lambda: back(x, x, w, s, s, out_index=i32), lambda: back(x, x, w, s, s, out=x[:5]), lambda: back(x, x, w, s, s, out=x, out_index=i32[:5]),
+        lambda: back(x, x, w, s, s, grad_dtype=torch.float16), lambda: back(x, x, w, s, s, accumulate_w=True),
+        lambda: back(x, x, w, s, s, grad_w=(w, w[:15])), lambda: back(x, x, w, s, s, workspace=x.t()),
+        lambda: tp.tppo_balance_loss(half, ids), lambda: tp.tppo_balance_loss(x, ids.long()), lambda: tp.tppo_balance_loss(x, ids[:5]),
+        lambda: tp.tppo_balance_loss(x, ids[:, 0]), lambda: tp.tppo_balance_loss(x, ids, out=(s[:1], None)),
+        lambda: tp.tppo_balance_loss(x, ids, out=(None, i32, None)), lambda: tp.tppo_balance_loss_backward(x, ids, counts_in=w),
+        lambda: tp.tppo_balance_loss_backward(x, ids, out_index=i32), lambda: tp.tppo_balance_loss_backward(x, ids, grad=x.bfloat16()),
+        lambda: tp.tppo_balance_loss_backward(x, ids, grad=x[:5]),
+        lambda: tp.tppo_orthogonalize(half), lambda: tp.tppo_orthogonalize(x.t()), lambda: tp.tppo_orthogonalize(w),
+        lambda: tp.tppo_orthogonalize(x, out=x), lambda: tp.tppo_orthogonalize(x, out=x[:5].bfloat16()),
+        lambda: tp.tppo_orthogonalize(x, coefficients=(1.0, 2.0)), lambda: tp.tppo_orthogonalize(x, out=x.bfloat16()[:1].expand(6, 16))]
+    for i, call in enumerate(calls):
+        with pytest.raises(ValueError):
+            call()
+            pytest.fail(f"call {i}")
+    for i, call in enumerate([
+            lambda: tp.tppo_layer_norm(x, w, eps=-1.0), lambda: back(x.bfloat16(), x, w, s, s), lambda: back(x, x, w, s, s, workspace=s),
+            lambda: tp.tppo_balance_loss(x, ids, coefficient=float("nan")), lambda: tp.tppo_balance_loss(x, ids, workspace=s),
+            lambda: tp.tppo_balance_loss_backward(x, ids, token_denominator=-1), lambda: tp.tppo_orthogonalize(x, steps=65),
+            lambda: tp.tppo_orthogonalize(x, workspace=s),
+            lambda: tp.tppo_orthogonalize(torch.zeros(2, 6, 16, device="cuda"), out=torch.zeros(1, 6, 16, dtype=BF, device="cuda").expand(2, 6, 16))]):
+        with pytest.raises(RuntimeError):
+            call()
+            pytest.fail(f"call {i}")
+
+
+def test_nothing_to_do():
+    x, w = torch.zeros(0, 16, device="cuda"), torch.ones(16, device="cuda")
+    ids = torch.zeros(0, 2, dtype=torch.int32, device="cuda")
+    y, mean, rstd = tp.tppo_layer_norm(x, w)
+    assert y.shape == (0, 16) and not bool(tp.tppo_layer_norm_backward(y, x, w, mean, rstd)[1].any())
+    grad, loss, counts, mean_prob = tp.tppo_balance_loss_backward(x, ids)
+    assert grad.shape == (0, 16) and float(loss) == 0 and not bool(counts.any()) and not bool(mean_prob.any())
+    assert tp.tppo_orthogonalize(torch.zeros(0, 6, 16, device="cuda")).shape == (0, 6, 16)
+    for shape in ((0, 16), (16, 0), (2, 0, 16)):
+        with pytest.raises(RuntimeError):
+            tp.tppo_orthogonalize(torch.zeros(shape, device="cuda"))
+
+
+def test_one_expert_and_one_element():
+    """The smallest of everything: E = 1 has a derivative of zero and a loss that is the coefficient."""
+    z, ids = torch.randn(300, 1, device="cuda"), torch.zeros(300, 1, dtype=torch.int32, device="cuda")
+    grad, loss, counts, mean_prob = tp.tppo_balance_loss_backward(z, ids, coefficient=0.5)
+    assert not bool(grad.any()) and float(loss) == 0.5 and counts.tolist() == [300] and mean_prob.tolist() == [1.0]
+    y, mean, rstd = tp.tppo_layer_norm(z, torch.ones(1, device="cuda"), torch.full((1,), 2.0, device="cuda"))
+    assert bool((y == 2).all()) and torch.equal(mean, z[:, 0])
+    for v in (3.0, -1e-3):
+        out = tp.tppo_orthogonalize(torch.full((1, 1), v, device="cuda"))
+        want = oops.orthogonalize(np.full((1, 1), np.float32(v)))
+        assert abs(float(out) - want) <= 2.0 ** -8 * abs(want)

@@ -424,48 +424,58 @@ __global__ __launch_bounds__(kNsThreads) void ns_begin_kernel(const T* __restric
     __shared__ double place[kNsThreads / kWave];
     __shared__ float tile[64][65];
     const int mat = blockIdx.y;
-    double sum = 0.0;
-    for (int i = threadIdx.x; i < count_parts; i += kNsThreads) sum += parts[(int64_t)mat * kNsParts + i];
-    sum = ns_workgroup_sum(sum, place);
-    const double norm = sqrt(sum) + (double)eps;
-    // growth: what the steps make of small singular values
-    const double most = sqrt(sum) / norm * growth;
-    const double lift = hi && most > 0.0 && most < 0.25 ? ldexp(1.0, -ilogb(most) - 3) : 1.0;
-    const double s_all = hi ? (double)s_scale * lift : (double)scale;
-    // (one of zeros with eps = 0 gives NaN, as 0 / 0 does; an infinity in G makes all of it NaN)
-    const double by = norm < 1.0e300 ? s_all / norm : __builtin_nan("");
-    if (hi && threadIdx.x == 0 && blockIdx.x == 0) scales[mat] = make_float2((float)(1.0 / (s_all * s_all)), (float)((double)scale / s_all));
     const T* from = g + mat * each;
     const int tiles_n = np / 64, tiles = tiles_n * (mp / 64);
+    double by = 0.0;
     for (int id = blockIdx.x; id < tiles; id += gridDim.x) {
         const int i0 = id / tiles_n * 64, j0 = (id - id / tiles_n * tiles_n) * 64;
-        if (transposed) {                            // G is [n, m]
-            const int lane = threadIdx.x & 63;
+        // all of a thread's entries are asked for at once, those of the first tile before the norm is added up: rows of G, or (G is [n, m])
+        // a column of 16 of its rows, which passes through LDS
+        float x[2][8];
+        if (transposed) {
+#pragma unroll
+            for (int k = 0; k < 16; ++k) {
+                const int r = (threadIdx.x >> 6) + k * 4, c = threadIdx.x & 63;
+                x[k >> 3][k & 7] = j0 + r < n && i0 + c < m ? to_f32(from[(int64_t)(j0 + r) * ld + i0 + c]) : 0.f;
+            }
+        } else {
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                const int i = i0 + half * 32 + (threadIdx.x >> 3), j = j0 + (threadIdx.x & 7) * 8;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) x[half][e] = 0.f;
+                if (i < m && j < n) get_piece<T, 8, true>(from + (int64_t)i * ld, j, n, x[half]);
+            }
+        }
+        if (id == (int)blockIdx.x) {
+            double sum = 0.0;
+            for (int i = threadIdx.x; i < count_parts; i += kNsThreads) sum += parts[(int64_t)mat * kNsParts + i];
+            sum = ns_workgroup_sum(sum, place);
+            const double norm = sqrt(sum) + (double)eps;
+            // growth: what the steps make of small singular values
+            const double most = sqrt(sum) / norm * growth;
+            const double lift = hi && most > 0.0 && most < 0.25 ? ldexp(1.0, -ilogb(most) - 3) : 1.0;
+            const double s_all = hi ? (double)s_scale * lift : (double)scale;
+            // (one of zeros with eps = 0 gives NaN, as 0 / 0 does; an infinity in G makes all of it NaN)
+            by = norm < 1.0e300 ? s_all / norm : __builtin_nan("");
+            if (hi && threadIdx.x == 0 && id == 0) scales[mat] = make_float2((float)(1.0 / (s_all * s_all)), (float)((double)scale / s_all));
+        }
+        if (transposed) {
             __syncthreads();
-#pragma unroll 4
-            for (int r = threadIdx.x >> 6; r < 64; r += 4)
-                tile[lane][r] = j0 + r < n && i0 + lane < m ? to_f32(from[(int64_t)(j0 + r) * ld + i0 + lane]) : 0.f;
+#pragma unroll
+            for (int k = 0; k < 16; ++k) tile[threadIdx.x & 63][(threadIdx.x >> 6) + k * 4] = x[k >> 3][k & 7];
             __syncthreads();
         }
 #pragma unroll
         for (int half = 0; half < 2; ++half) {       // eight columns of a row
             const int r = half * 32 + (threadIdx.x >> 3), c = (threadIdx.x & 7) * 8, i = i0 + r, j = j0 + c;
-            float x[8];
-            if (transposed) {
 #pragma unroll
-                for (int e = 0; e < 8; ++e) x[e] = tile[r][c + e];
-            } else {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) x[e] = 0.f;
-                if (i < m && j < n) get_piece<T, 8, true>(from + (int64_t)i * ld, j, n, x);
-            }
-#pragma unroll
-            for (int e = 0; e < 8; ++e) x[e] = (float)((double)x[e] * by);
+            for (int e = 0; e < 8; ++e) x[half][e] = (float)((double)(transposed ? tile[r][c + e] : x[half][e]) * by);
             if (hi) {
                 half8 h, l;
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
-                    const float y = i < m && j + e < n ? x[e] : 0.f;                           // (zeros, also where `by` is no number)
+                    const float y = i < m && j + e < n ? x[half][e] : 0.f;                     // (zeros, also where `by` is no number)
                     h[e] = (half_t)y;
                     l[e] = (half_t)((y - (float)h[e]) * kLoScale);
                 }
@@ -475,7 +485,7 @@ __global__ __launch_bounds__(kNsThreads) void ns_begin_kernel(const T* __restric
             } else {
 #pragma unroll
                 for (int e = 0; e < 8; ++e)
-                    if (i < m && j + e < n) out[mat * each_out + (transposed ? (int64_t)(j + e) * ld_out + i : (int64_t)i * ld_out + j + e)] = ns_bf16(x[e]);
+                    if (i < m && j + e < n) out[mat * each_out + (transposed ? (int64_t)(j + e) * ld_out + i : (int64_t)i * ld_out + j + e)] = ns_bf16(x[half][e]);
             }
         }
     }

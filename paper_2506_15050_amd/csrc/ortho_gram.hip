@@ -14,7 +14,7 @@ namespace tppo {
 constexpr float kPolyScale = 16.f;                   // of P, whose eigenvalues go up to a^steps
 constexpr int kPairThreads = 256, kPairTile = 64, kPairStage = 4 * kPairTile * 128;
 
-enum PairMode { kPairGram, kPairPoly, kPairMul, kPairLast };
+enum PairMode { kPairGram, kPairWhole, kPairPoly, kPairMul, kPairLast };        // X X^T: partial sums of it; all of it, as pairs
 
 // One product of pairs, out[t, v] = sum_k t_op[t, k] v_op[v, k] (kPairLast: v_op[k, v]).
 struct PairProblem {
@@ -83,7 +83,7 @@ __device__ __forceinline__ void pair_store(const float (*tile)[kTileLd], int t0,
 template <PairMode MODE, int STAGES>
 __global__ __launch_bounds__(kPairThreads, STAGES == 2 ? 2 : 1) void ns_pair_kernel(PairArgs p) {
     extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
-    constexpr bool kKMajor = MODE == kPairLast;
+    constexpr bool kKMajor = MODE == kPairLast, kBothX = MODE == kPairGram || MODE == kPairWhole;
     // chunk by chunk, or V tile by V tile, of a tile, tile by tile, matrix by matrix, problem by problem; consecutive ones on an XCD, whose L2
     // holds a small matrix (eight of 333 rows spread over all: 174 -> 183 us a call)
     int rest = ns_by_xcd(blockIdx.x, gridDim.x), inner, tile, mat;
@@ -163,8 +163,8 @@ __global__ __launch_bounds__(kPairThreads, STAGES == 2 ? 2 : 1) void ns_pair_ker
 #pragma unroll
                 for (int tb = 0; tb < 2; ++tb) {
                     acc[vb][tb] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v[0][vb], t[0][tb], acc[vb][tb], 0, 0, 0);
-                    f32x4& with_t = MODE == kPairGram ? cross[vb][tb] : acc[vb][tb];           // (X's low halves are scaled)
-                    f32x4& with_v = MODE == kPairGram || MODE == kPairLast ? cross[vb][tb] : acc[vb][tb];
+                    f32x4& with_t = kBothX ? cross[vb][tb] : acc[vb][tb];                      // (X's low halves are scaled)
+                    f32x4& with_v = kBothX || MODE == kPairLast ? cross[vb][tb] : acc[vb][tb];
                     with_t = __builtin_amdgcn_mfma_f32_16x16x32_f16(v[0][vb], t[1][tb], with_t, 0, 0, 0);
                     with_v = __builtin_amdgcn_mfma_f32_16x16x32_f16(v[1][vb], t[0][tb], with_v, 0, 0, 0);
                 }
@@ -181,7 +181,7 @@ __global__ __launch_bounds__(kPairThreads, STAGES == 2 ? 2 : 1) void ns_pair_ker
             float x[4];
 #pragma unroll
             for (int e = 0; e < 4; ++e)
-                x[e] = MODE == kPairGram || MODE == kPairLast ? fmaf(cross[vb][tb][e], 1.f / kLoScale, acc[vb][tb][e]) : acc[vb][tb][e];
+                x[e] = kBothX || MODE == kPairLast ? fmaf(cross[vb][tb][e], 1.f / kLoScale, acc[vb][tb][e]) : acc[vb][tb][e];
             if constexpr (MODE == kPairGram) {
                 *reinterpret_cast<float4*>(p.part + ((int64_t)chunk * p.count + mat) * p.each_out + (int64_t)t * p.ld_out + v) =
                     make_float4(x[0], x[1], x[2], x[3]);
@@ -198,7 +198,7 @@ __global__ __launch_bounds__(kPairThreads, STAGES == 2 ? 2 : 1) void ns_pair_ker
                 }
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    float y = x[e] * q.in_scale;
+                    float y = x[e] * (MODE == kPairWhole ? p.scales[mat].x : q.in_scale);
                     if constexpr (MODE == kPairPoly)
                         y = fmaf(p.x.c, y, fmaf(p.x.b * (1.f / kOffScale), (float)a_hi[e] + (float)a_lo[e], t == v + e ? p.x.a : 0.f));
                     tile_out[t - t0][v - v0 + e] = y * q.out_scale;
@@ -220,7 +220,7 @@ __global__ __launch_bounds__(kPairThreads, STAGES == 2 ? 2 : 1) void ns_pair_ker
                 put_whole_or_part(p.x.out + mat * p.x.each_out + (int64_t)row_at * p.x.ld_out + col_at, cols - col_at, x);
         }
     }
-    if constexpr (MODE == kPairPoly || MODE == kPairMul) {
+    if constexpr (MODE == kPairWhole || MODE == kPairPoly || MODE == kPairMul) {
         __syncthreads();
         pair_store(tile_out, t0, v0, q.out_hi + mat * p.each_out, q.out_lo + mat * p.each_out, p.ld_out);
     }
@@ -468,6 +468,8 @@ bool ns_gram_fits(int steps, float a, float b, float c) {
 }
 
 namespace {
+constexpr int kIterateMost = 128;                    // rows of what ns_iterate_kernel takes
+constexpr int64_t kGatherStages = 11;
 struct GramLayout {
     int tiles, chunks;
     size_t part, m[2], p[2], a, t, total;            // pairs: hi, then lo
@@ -476,9 +478,12 @@ GramLayout gram_layout(int64_t count, int mp, int np) {
     GramLayout L;
     const int side = mp / kPairTile;
     L.tiles = side * (side + 1) / 2;
-    // contractions are cut until there are two workgroups to a CU, each with four stages at least
+    // contractions are cut until there are two workgroups to a CU, each with four stages at least; not where that saves no more stages than
+    // the launch that gathers the parts takes.  us, cut / whole:  512 x 512, 8 stages in 2 parts: 152.7 / 150.3;  8 x 1000 x 333, 16 in 3: 167.7 /
+    // 164.3;  512 x 1024, 16 in 4: 152.0 / 154.1;  333 x 2048, 32 in 8: 130.7 / 139.1
     const int64_t all = (int64_t)L.tiles * count, stages = np / 64;
     L.chunks = (int)std::max<int64_t>(1, std::min<int64_t>(stages / 4, 512 / all));
+    if (mp > kIterateMost && stages - stages / L.chunks <= kGatherStages) L.chunks = 1;
     size_t o = 0;
     auto take = [&](size_t bytes) {
         const size_t at = o;
@@ -486,7 +491,7 @@ GramLayout gram_layout(int64_t count, int mp, int np) {
         return at;
     };
     const size_t pair = (size_t)count * mp * mp * 4;
-    L.part = take((size_t)L.chunks * count * mp * mp * 4);
+    L.part = take(mp > kIterateMost && L.chunks == 1 ? 0 : (size_t)L.chunks * count * mp * mp * 4);
     for (size_t* at : {&L.m[0], &L.m[1], &L.p[0], &L.p[1], &L.a, &L.t}) *at = take(pair);
     L.total = o;
     return L;
@@ -538,7 +543,13 @@ int ns_gram(const NsShape& x, const half_t* hi, const half_t* lo, const float2* 
     p.tiles = L.tiles;
     p.stages = np / 64;
     p.chunks = L.chunks;
-    if (launch_pair<kPairGram>(p, 1, s) != TPPO_OK) return TPPO_ERR_LAUNCH;
+    const bool whole = mp > kIterateMost && L.chunks == 1;
+    if (whole) {
+        p.problem[0] = {hi, lo, hi, lo, A, A + half, 1.f, kOffScale};
+        if (launch_pair<kPairWhole>(p, 1, s) != TPPO_OK) return TPPO_ERR_LAUNCH;
+    } else if (launch_pair<kPairGram>(p, 1, s) != TPPO_OK) {
+        return TPPO_ERR_LAUNCH;
+    }
     if (L.chunks > kFewChunks) {
         const int64_t quads = half / 4;
         hipLaunchKernelGGL(ns_reduce_kernel, dim3((unsigned)(quads / 64)), dim3(256), 0, s, reinterpret_cast<float4*>(p.part), L.chunks, quads);
@@ -546,11 +557,12 @@ int ns_gram(const NsShape& x, const half_t* hi, const half_t* lo, const float2* 
     }
     half_t* P = pair(L.p[0]);
     float p_scale = kPolyScale;
-    if (mp <= 128) {
+    if (mp <= kIterateMost) {
         if ((mp == 64 ? launch_iterate<64>(p, P, P + half, s) : launch_iterate<128>(p, P, P + half, s)) != TPPO_OK) return TPPO_ERR_LAUNCH;
     } else {
-        hipLaunchKernelGGL(ns_gather_kernel, dim3((unsigned)L.tiles, (unsigned)x.count), dim3(256), 0, s, p.part, p.chunks, p.count, mp,
-                           scales, A, A + half);
+        if (!whole)
+            hipLaunchKernelGGL(ns_gather_kernel, dim3((unsigned)L.tiles, (unsigned)x.count), dim3(256), 0, s, p.part, p.chunks, p.count, mp,
+                               scales, A, A + half);
         p.chunks = 1;
         p.stages = mp / 64;
         p.each_t = p.each_v = each;

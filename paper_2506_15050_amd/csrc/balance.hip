@@ -341,15 +341,19 @@ __global__ __launch_bounds__(kBlLast) void balance_finish_kernel(Balance b) {
         if (n > 0.0) loss = (double)(b.counts_in ? b.counts_in[e] : (int64_t)c) / ((double)b.k * n) * p;
     }
     loss = wave_prefix(loss);
-    if (threadIdx.x == kWave - 1 && b.loss) {
+    if (!b.loss) return;
+    int last = 0;
+    if (threadIdx.x == kWave - 1) {
         __hip_atomic_store(b.part_loss + blockIdx.x, loss, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
         __threadfence();
-        if (atomicAdd(b.arrived, 1) + 1 == (int)gridDim.x) {
-            __threadfence();
-            double all = 0.0;
-            for (int w = 0; w < (int)gridDim.x; ++w) all += __hip_atomic_load(b.part_loss + w, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-            *b.loss = (float)((double)b.coefficient * E * all);
-        }
+        last = atomicAdd(b.arrived, 1) + 1 == (int)gridDim.x;
+    }
+    if (__builtin_amdgcn_readlane(last, kWave - 1)) {
+        __threadfence();
+        static_assert(kBlMaxE / kBlColumns <= kWave, "a workgroup's loss to a lane");
+        double all = threadIdx.x < gridDim.x ? __hip_atomic_load(b.part_loss + threadIdx.x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : 0.0;
+        all = wave_prefix(all);
+        if (threadIdx.x == kWave - 1) *b.loss = (float)((double)b.coefficient * E * all);
     }
 }
 

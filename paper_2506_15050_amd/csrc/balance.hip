@@ -359,6 +359,10 @@ __global__ __launch_bounds__(kBlLast) void balance_finish_kernel(Balance b) {
 
 // Lanes of a row for so many pieces: 4, 8 or 16, and 64 beyond 64 pieces.
 static int lanes_of(int64_t pieces) { return pieces <= 4 ? 4 : pieces <= 8 ? 8 : pieces <= 64 ? 16 : 64; }
+static int pieces_of_lane(int64_t pieces) {          // rounded up to a power of two, as launch_rows has them
+    const int64_t each = (pieces + lanes_of(pieces) - 1) / lanes_of(pieces);
+    return each <= 1 ? 1 : each <= 2 ? 2 : each <= 4 ? 4 : 8;
+}
 
 template <class T, bool GRAD>
 static void launch_rows(const Balance& b, hipStream_t s) {
@@ -393,12 +397,15 @@ static void launch_rows(const Balance& b, hipStream_t s) {
 }
 
 // Workgroups of the rows' kernel: up to kBlGroups, as many as have rows for all their lanes; one alone where that has no more than
-// kBlAlone pieces a thread and so many choices, whose work is less than the two or three launches that it does without.
+// kBlAlone pieces a thread and so many choices, whose work is less than the two or three launches that it does without.  Derivatives of 32
+// columns a thread leave registers for one workgroup to a CU, and one round of those is the shorter: 512 / 256 workgroups, us:  8000 x 2048, fp32:
+// 59.8 / 50.3, bf16: 50.0 / 41.0;  20000 x 512, bf16: 33.5 / 30.5;  where two fit:  10000 x 1024, fp32: 32.5 / 36.0.
 constexpr int64_t kBlAlone = 8;
-static int row_groups(int64_t M, int64_t k, int64_t E, int per_piece) {
+static int row_groups(int64_t M, int64_t k, int64_t E, int per_piece, bool grad) {
     const int64_t pieces = (E + per_piece - 1) / per_piece, rows = kBlThreads / lanes_of(pieces), want = (M + rows - 1) / rows;
     if (M * pieces <= kBlAlone * kBlThreads && M * k <= kBlAlone * kBlThreads) return 1;
-    return (int)(want < 2 ? 2 : want < kBlGroups ? want : kBlGroups);
+    const int most = grad && pieces_of_lane(pieces) * per_piece >= 32 ? kBlGroups / 2 : kBlGroups;
+    return (int)(want < 2 ? 2 : want < most ? want : most);
 }
 
 static int check(const Balance& b, tppo_dtype dt) {
@@ -422,7 +429,7 @@ static size_t part_bytes(int64_t E, int rows) { return round_up((size_t)rows * E
 static int run_balance(Balance& b, tppo_dtype dt, bool grad, void* workspace, size_t workspace_bytes, hipStream_t s) {
     if (!workspace || !is_aligned(workspace, 256) || workspace_bytes < tppo_balance_loss_workspace_bytes(b.M, b.E))
         return TPPO_ERR_WORKSPACE;
-    b.groups = row_groups(b.M, b.k, b.E, dt == TPPO_F32 ? 4 : 8);
+    b.groups = row_groups(b.M, b.k, b.E, dt == TPPO_F32 ? 4 : 8, grad);
     char* ws = static_cast<char*>(workspace);
     b.part_p = reinterpret_cast<float*>(ws);
     b.part_counts = reinterpret_cast<int32_t*>(ws + part_bytes(b.E, kBlGroups));

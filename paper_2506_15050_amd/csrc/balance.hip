@@ -4,7 +4,9 @@
 //     d loss / d logits[m, i] = coefficient E / N * p_i (f_i - sum_e f_e p_e)
 // The p of a row add up to one, so f may be taken from its mean over the experts, d_e = (counts_e - total / E) / (k N): an even use,
 // where all f_e are alike, loses no digits to the difference.
-// Bound by memory: every logit is read once and, backward, every derivative written once.
+// Bound by memory: every logit is read once and, backward, every derivative written once; and by two or three launches that wait for each
+// other, 10 to 16 us whatever the size.  Backward of 77536 x 128, fp32: 30 us, of which the choices 6.5, the rows 17 (4.7 TB/s) and the
+// finishing kernel 5;  2000 x 128: 16;  forward of 77536 x 256: 24.5, rows and choices 17, finishing 5.5;  146 x 8, all in one launch: 4.
 #include "rows.h"
 
 namespace tppo {
@@ -123,7 +125,9 @@ __device__ __forceinline__ double workgroup_sum(double x, double* place) {
 }
 
 // kLanes lanes a row, kPieces pieces of 16 bytes for each, kAtOnce rows under way.  GRAD: derivatives are written, from counts that are
-// there already; otherwise the workgroup counts its part of the choices as well.  ONE: a single workgroup, which does all of the call.
+// there already; otherwise the workgroup counts its part of the choices as well (by workgroups of their own in the same launch: 77536 x 256
+// 24.5 -> 28 us).  ONE: a single workgroup, which does all of the call.  Asking for a turn's rows before the one before is worked on gained
+// nothing at 22 sizes: there are workgroups enough to cover for each other.
 // Sums over a row are log2(kLanes) steps for 64 / kLanes rows side by side, so lanes are few and have several pieces as long as registers
 // for the columns' sums and counts (2 kPieces kN) are no matter.
 template <class T, int kLanes, int kPieces, bool RAGGED, bool GRAD, bool ONE>

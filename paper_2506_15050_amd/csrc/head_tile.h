@@ -916,7 +916,7 @@ static_assert(64 * 16 >= kSweepGroups * sizeof(int32_t), "a word for every workg
 
 // A kernel that wants more than 64 KiB of LDS has to be told so once per device.
 static bool allow_lds(const void* fn, int lds_bytes) {
-    constexpr int kMaxDevices = 64, kMaxKernels = 32;
+    constexpr int kMaxDevices = 64, kMaxKernels = 16;
     static std::atomic<const void*> done[kMaxDevices][kMaxKernels];
     int dev = -1;
     if (hipGetDevice(&dev) != hipSuccess || dev < 0) return false;

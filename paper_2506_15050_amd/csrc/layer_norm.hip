@@ -32,6 +32,8 @@ __device__ __forceinline__ void row_sums(float& a, float& b, float2 (*place)[kLa
 
 // Forward.  kLanes threads a row, kPieces pieces of 16 bytes for each, which stay in registers: the row is read once, the mean and then
 // the sum of squared differences from it are taken from there (no difference of large numbers).
+// Bound by memory: 77536 x 5120, bf16: 265 us, 6.0 TB/s, where a plain pass over as many streams reaches 6.2 to 6.4 (kept in the caches on
+// the way, 275).  63 x 64: 3 us, the latency of a launch and two dependent loads.
 template <class T, class W, int kLanes, int kPieces, bool RAGGED>
 __global__ __launch_bounds__(kLnThreads) void layer_norm_kernel(
     const T* __restrict__ x, int64_t n_rows, int H, int64_t ld_x, const W* __restrict__ weight, const W* __restrict__ bias, float eps,
@@ -105,6 +107,8 @@ __global__ __launch_bounds__(kLnThreads) void layer_norm_kernel(
 // Backward.  kLanes threads a row as above; the two sums of a row are taken together, and the next row is asked for before this one is
 // worked on.  A thread's columns are the same in all of its rows, so it adds up their weights' derivatives in registers; the groups of a
 // workgroup add theirs in LDS, and each workgroup leaves one row of partial sums, [2][H], which add_rows_kernel adds in a fixed order.
+// Bound by memory: a call of 19384 x 5120, bf16 with fp32 grad_y: 152 us, 5.2 TB/s, 6 of them add_rows_kernel (without the next row asked for
+// 187); 16416 x 1024, fp32: 45 us, 4.4 TB/s, 5 of them add_rows_kernel; 2513 x 1001, bf16: 13.5, two launches' latency.
 // Wavefronts that a SIMD's 512 registers hold: a thread's weights and two sums for each of its columns, and two rows of both inputs.
 template <class T, class G, int kPieces>
 constexpr int backward_waves() {

@@ -2,6 +2,8 @@
 //     X = G / (|G|_F + eps), wide;   steps times:  A = X X^T,  B = b A + c A A,  X = a X + B X
 // Three matrix products a step on the matrix cores, 2 m (m n + m m + m n) flop, of which the first two have symmetric results: only the
 // tiles on and below the diagonal are computed, and written twice.
+// Bound by the matrix cores: 5120 x 5120, 5 steps: 2600 us, 1.03 PFLOP/s of the flops that are needed; 1.45 within a round of tiles, as a
+// large library product reaches, of which X X^T and A A fill 82 % of the CUs and B X two rounds by 78 %.
 //
 // Precision.  A rounding of X is a matrix with singular values in every direction, and the iteration multiplies small ones by up to a
 // each time, a^steps = 485 in all: bf16 operands turn a gradient of rank one into noise (error 1.2 of 1), fp16 ones still 0.15.  So

@@ -3,6 +3,8 @@
 //     M = a I + b A + c A A,   A <- M A M,   P <- M P;   at the end X = P X_0.
 // X is read twice instead of twice a step, and what is left between is m x m: 6 m^2 n + 17 m^3 flop (5 steps, halves of symmetric
 // results not counted) against 15 m^2 n + 5 m^3.
+// Bound by the chain of products that wait for each other: 64 x 1024: 30.6 us (norm 3, first X 4, X X^T 5, all steps 15.5, P X 4); eight of
+// 1000 x 333: 163, of which 14 products of 7 to 10.
 // Precision.  A holds squares of singular values, and its errors where they are small grow by a^2 a step.  So everything here is a pair of
 // fp16, hi + lo, rounded to nearest, 22 bits of what is not far below 1, products are hi hi + hi lo + lo hi with sums in fp32, and A is made
 // symmetric to the bit, step by step.  Emulated against 64 bits: 1.6e-3 of the result's norm at worst (2 x 3, singular values 1 and 0.01), 1e-3
@@ -259,7 +261,7 @@ __global__ __launch_bounds__(256) void ns_gather_kernel(const float* part, int c
 // product (M A, then M (M A)); as the matrices are symmetric the other operand, all rows of A or M, is every wavefront's strip as well, and
 // passes through LDS once a step each, in the order of the lanes.  Only the new A is exchanged across the diagonal, where it is
 // made the mean of both sides.
-// Bound by the chain of products: 17 for 5 steps, 24 MFMAs a wavefront each (192 at 128 rows).  64 rows, us: blocks of lower triangles
+// Bound by the chain of products: 17 for 5 steps, 24 MFMAs a wavefront each (192 at 128 rows).  64 rows, us: so, 15.5; blocks of lower triangles
 // dealt out to 16 wavefronts, mirrored in LDS by pieces of two bytes, 16.5; all blocks where they lie, operands from LDS, 16 wavefronts 20.7,
 // four 26.5.
 constexpr int kIterThreads = 256;

@@ -566,8 +566,8 @@ int tppo_balance_loss_backward(const void* logits, int64_t n_rows, int64_t E, in
 
 /* ---------------------------------------------------------------------------
  * tppo_orthogonalize -- an update (a weight matrix's gradient or momentum) made
- * nearly orthogonal by Newton-Schulz products, what the Muon optimiser applies
- * to hidden matrices.  For each of `count` matrices G, with X the wide one of G
+ * nearly orthogonal by Newton-Schulz products, what optimisers apply to hidden
+ * matrices instead of an elementwise scale.  For each of `count` matrices G, with X the wide one of G
  * and its transpose:
  *   X = G / (|G|_F + eps)
  *   `steps` times:  A = X X^T;  X = a X + (b A + c A^2) X

@@ -255,95 +255,100 @@ __global__ __launch_bounds__(256) void ns_gather_kernel(const float* part, int c
     pair_store(tile, t0, v0, hi + (int64_t)mat * mp * mp, lo + (int64_t)mat * mp * mp, mp);
 }
 
-// All steps of one matrix of up to MP = 64 or 128 rows in one workgroup of four wavefronts, each with a strip of columns of every matrix.
+// All steps of one matrix of up to MP = 64 or 128 rows in one workgroup, a strip of 16 columns of every matrix to a wavefront.
 // A block of 16 x 16 comes out of an MFMA as it goes into one: lane l has column l % 16 and rows 4 (l / 16) .. + 3, and two blocks are the
 // 32 of K of the next one's operand, in an order of their own, the same on both sides.  So a strip stays in registers from product to
 // product (M A, then M (M A)); as the matrices are symmetric the other operand, all rows of A or M, is every wavefront's strip as well, and
 // passes through LDS once a step each, in the order of the lanes.  Only the new A is exchanged across the diagonal, where it is
 // made the mean of both sides.
-// Bound by the chain of products: 17 for 5 steps, 24 MFMAs a wavefront each (192 at 128 rows).  64 rows, us: so, 15.5; blocks of lower triangles
-// dealt out to 16 wavefronts, mirrored in LDS by pieces of two bytes, 16.5; all blocks where they lie, operands from LDS, 16 wavefronts 20.7,
-// four 26.5.
-constexpr int kIterThreads = 256;
+// Bound by the chain of products: 17 for 5 steps, 24 MFMAs a wavefront each (96 at 128 rows), and by LDS, which every wavefront reads whole.
+// 64 rows, us: so, 12; blocks of lower triangles dealt out to 16 wavefronts, mirrored in LDS by pieces of two bytes, 16.5; all blocks where
+// they lie, operands from LDS, 16 wavefronts 20.7, four 26.5.  A call with 128 x 1024: 61; two strips to each of four wavefronts 68; sums read
+// where each lane wants them, across the diagonal, 117.
 template <int MP>
-__global__ __launch_bounds__(kIterThreads, 1) void ns_iterate_kernel(const float* part, int chunks, int count, const float2* scales, int steps,
+__global__ __launch_bounds__(MP * 4, MP / 64) void ns_iterate_kernel(const float* part, int chunks, int count, const float2* scales, int steps,
                                                                      float a, float b, float c, half_t* p_hi, half_t* p_lo) {
-    constexpr int kB = MP / 16, kT = MP / 64, kPairs = kB / 2;       // blocks of a column; of a strip's width; operands of 32 of K
+    constexpr int kThreads = MP * 4, kB = MP / 16, kPairs = kB / 2;                   // blocks of a column; operands of 32 of K
     constexpr int kOperand = kB * kPairs * 2 * 1024, kTurnLd = MP + 1;
     extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
     unsigned char *const all_m = smem, *const all_a = smem + kOperand;
     float* const turned = reinterpret_cast<float*>(all_a);           // (MP x kTurnLd, when A has been read)
     const int mat = blockIdx.x, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int col = lane & 15, grp = lane >> 4, strip = wave * kT * 16;
-    typedef f32x4 Strip[kB][kT];
+    const int col = lane & 15, grp = lane >> 4, t = wave * 16 + col;
+    typedef f32x4 Strip[kB];
     struct Pairs {
-        half8 hi[kPairs][kT], lo[kPairs][kT];
+        half8 hi[kPairs], lo[kPairs];
     };
     Strip A, M, S;
     Pairs pa, pm, pp;
     const float by = scales[mat].x * kOffScale;
+    {   // the parts' sum, in whole pieces and through LDS (there are sums on and above the diagonal)
+        constexpr int kPieces = MP * MP / 4 / kThreads;
+        float4 sum[kPieces];
 #pragma unroll
-    for (int j = 0; j < kB; ++j)
-#pragma unroll
-        for (int i = 0; i < kT; ++i) A[j][i] = f32x4{0, 0, 0, 0};
-    // (a chunk's sums all asked for at once; there are sums on and above the diagonal)
+        for (int q = 0; q < kPieces; ++q) sum[q] = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 2
-    for (int k = 0; k < chunks; ++k) {
-        const float* at = part + ((int64_t)k * count + mat) * MP * MP;
+        for (int k = 0; k < chunks; ++k) {
+            const float4* at = reinterpret_cast<const float4*>(part + ((int64_t)k * count + mat) * MP * MP) + threadIdx.x;
+#pragma unroll
+            for (int q = 0; q < kPieces; ++q) {
+                const float4 x = at[q * kThreads];
+                sum[q].x += x.x; sum[q].y += x.y; sum[q].z += x.z; sum[q].w += x.w;
+            }
+        }
+#pragma unroll
+        for (int q = 0; q < kPieces; ++q) {
+            const int at = (q * kThreads + (int)threadIdx.x) * 4;
+            float* to = turned + at / MP * kTurnLd + at % MP;
+            to[0] = sum[q].x; to[1] = sum[q].y; to[2] = sum[q].z; to[3] = sum[q].w;
+        }
+        __syncthreads();
 #pragma unroll
         for (int j = 0; j < kB; ++j)
 #pragma unroll
-            for (int i = 0; i < kT; ++i) {
-                const int t = strip + i * 16 + col, v = j * 16 + grp * 4;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) A[j][i][e] += at[min(t, v + e) * MP + max(t, v + e)];
+            for (int e = 0; e < 4; ++e) {
+                const int v = j * 16 + grp * 4 + e;
+                A[j][e] = turned[min(t, v) * kTurnLd + max(t, v)] * by;
             }
+        __syncthreads();
     }
-#pragma unroll
-    for (int j = 0; j < kB; ++j)
-#pragma unroll
-        for (int i = 0; i < kT; ++i) A[j][i] *= by;
     auto split = [&](const Strip& x, Pairs& p) {
         typedef float f2 __attribute__((ext_vector_type(2)));
         typedef half_t h2 __attribute__((ext_vector_type(2)));
 #pragma unroll
         for (int j = 0; j < kB; ++j)
 #pragma unroll
-            for (int i = 0; i < kT; ++i)
-#pragma unroll
-                for (int e = 0; e < 4; e += 2) {
-                    const f2 y = {x[j][i][e], x[j][i][e + 1]};
-                    const h2 h = __builtin_convertvector(y, h2);
-                    const f2 rest = {y[0] - (float)h[0], y[1] - (float)h[1]};
-                    const h2 l = __builtin_convertvector(rest, h2);
-                    const int at = (j & 1) * 4 + e;
-                    p.hi[j >> 1][i][at] = h[0];
-                    p.hi[j >> 1][i][at + 1] = h[1];
-                    p.lo[j >> 1][i][at] = l[0];
-                    p.lo[j >> 1][i][at + 1] = l[1];
-                }
+            for (int e = 0; e < 4; e += 2) {
+                const f2 y = {x[j][e], x[j][e + 1]};
+                const h2 h = __builtin_convertvector(y, h2);
+                const f2 rest = {y[0] - (float)h[0], y[1] - (float)h[1]};
+                const h2 l = __builtin_convertvector(rest, h2);
+                const int at = (j & 1) * 4 + e;
+                p.hi[j >> 1][at] = h[0];
+                p.hi[j >> 1][at + 1] = h[1];
+                p.lo[j >> 1][at] = l[0];
+                p.lo[j >> 1][at + 1] = l[1];
+            }
     };
     // this strip as rows of the other operand
     auto publish = [&](unsigned char* all, const Pairs& p) {
 #pragma unroll
-        for (int i = 0; i < kT; ++i)
-#pragma unroll
-            for (int j = 0; j < kPairs; ++j) {
-                half8* at = reinterpret_cast<half8*>(all + (((wave * kT + i) * kPairs + j) * 2) * 1024) + lane;
-                at[0] = p.hi[j][i];
-                at[64] = p.lo[j][i];
-            }
+        for (int j = 0; j < kPairs; ++j) {
+            half8* at = reinterpret_cast<half8*>(all + ((wave * kPairs + j) * 2) * 1024) + lane;
+            at[0] = p.hi[j];
+            at[64] = p.lo[j];
+        }
     };
-    // (chains of MFMAs on one sum side by side: four rows of blocks at a time)
+    // (chains of MFMAs on one sum side by side: four rows of blocks at a time; at 128 rows no operand is asked for further ahead, or they all
+    // are, which takes 221 registers more than there are)
     auto product = [&](const unsigned char* all, const Pairs& p, Strip& out) {
 #pragma unroll
         for (int r0 = 0; r0 < kB; r0 += 4) {
 #pragma unroll
-            for (int r = r0; r < r0 + 4; ++r)
-#pragma unroll
-                for (int i = 0; i < kT; ++i) out[r][i] = f32x4{0, 0, 0, 0};
+            for (int r = r0; r < r0 + 4; ++r) out[r] = f32x4{0, 0, 0, 0};
 #pragma unroll
             for (int j = 0; j < kPairs; ++j) {
+                if constexpr (MP > 64) __builtin_amdgcn_sched_barrier(0);
                 half8 hi[4], lo[4];
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
@@ -355,10 +360,7 @@ __global__ __launch_bounds__(kIterThreads, 1) void ns_iterate_kernel(const float
                 for (int part = 0; part < 3; ++part)
 #pragma unroll
                     for (int r = 0; r < 4; ++r)
-#pragma unroll
-                        for (int i = 0; i < kT; ++i)
-                            out[r0 + r][i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(part < 2 ? hi[r] : lo[r], part == 1 ? p.lo[j][i] : p.hi[j][i],
-                                                                                   out[r0 + r][i], 0, 0, 0);
+                        out[r0 + r] = __builtin_amdgcn_mfma_f32_16x16x32_f16(part < 2 ? hi[r] : lo[r], part == 1 ? p.lo[j] : p.hi[j], out[r0 + r], 0, 0, 0);
             }
         }
     };
@@ -373,18 +375,13 @@ __global__ __launch_bounds__(kIterThreads, 1) void ns_iterate_kernel(const float
 #pragma unroll
         for (int j = 0; j < kB; ++j)
 #pragma unroll
-            for (int i = 0; i < kT; ++i)
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    M[j][i][e] = fmaf(c * (1.f / (kOff * kOff)), S[j][i][e],
-                                      fmaf(b * (1.f / kOff), A[j][i][e], strip + i * 16 + col == j * 16 + grp * 4 + e ? a : 0.f));
+            for (int e = 0; e < 4; ++e)
+                M[j][e] = fmaf(c * (1.f / (kOff * kOff)), S[j][e], fmaf(b * (1.f / kOff), A[j][e], t == j * 16 + grp * 4 + e ? a : 0.f));
         split(M, pm);
         publish(all_m, pm);
         if (step == 0) {
 #pragma unroll
-            for (int j = 0; j < kB; ++j)
-#pragma unroll
-                for (int i = 0; i < kT; ++i) M[j][i] *= kPolyScale;
+            for (int j = 0; j < kB; ++j) M[j] *= kPolyScale;
             split(M, pp);
         }
         __syncthreads();                                             // all of M is there; A has been read
@@ -399,31 +396,24 @@ __global__ __launch_bounds__(kIterThreads, 1) void ns_iterate_kernel(const float
 #pragma unroll
         for (int j = 0; j < kB; ++j)
 #pragma unroll
-            for (int i = 0; i < kT; ++i)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) turned[(j * 16 + grp * 4 + e) * kTurnLd + strip + i * 16 + col] = S[j][i][e];
+            for (int e = 0; e < 4; ++e) turned[(j * 16 + grp * 4 + e) * kTurnLd + t] = S[j][e];
         __syncthreads();                                             // and M has been read
 #pragma unroll
         for (int j = 0; j < kB; ++j)
 #pragma unroll
-            for (int i = 0; i < kT; ++i)
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    A[j][i][e] = (S[j][i][e] + turned[(strip + i * 16 + col) * kTurnLd + j * 16 + grp * 4 + e]) * 0.5f;
+            for (int e = 0; e < 4; ++e) A[j][e] = (S[j][e] + turned[t * kTurnLd + j * 16 + grp * 4 + e]) * 0.5f;
         split(A, pa);
         __syncthreads();
         publish(all_a, pa);
         __syncthreads();
     }
 #pragma unroll
-    for (int i = 0; i < kT; ++i)
-#pragma unroll
-        for (int j = 0; j < kB; ++j) {
-            const int64_t at = ((int64_t)mat * MP + strip + i * 16 + col) * MP + j * 16 + grp * 4;
-            const half8 h = pp.hi[j >> 1][i], l = pp.lo[j >> 1][i];
-            *reinterpret_cast<half4*>(p_hi + at) = j & 1 ? half4{h[4], h[5], h[6], h[7]} : half4{h[0], h[1], h[2], h[3]};
-            *reinterpret_cast<half4*>(p_lo + at) = j & 1 ? half4{l[4], l[5], l[6], l[7]} : half4{l[0], l[1], l[2], l[3]};
-        }
+    for (int j = 0; j < kB; ++j) {
+        const int64_t at = ((int64_t)mat * MP + t) * MP + j * 16 + grp * 4;
+        const half8 h = pp.hi[j >> 1], l = pp.lo[j >> 1];
+        *reinterpret_cast<half4*>(p_hi + at) = j & 1 ? half4{h[4], h[5], h[6], h[7]} : half4{h[0], h[1], h[2], h[3]};
+        *reinterpret_cast<half4*>(p_lo + at) = j & 1 ? half4{l[4], l[5], l[6], l[7]} : half4{l[0], l[1], l[2], l[3]};
+    }
 }
 
 // Partial sums of many chunks into the first one's place: 64 float4 a workgroup, its four wavefronts a quarter of the chunks each.
@@ -517,7 +507,7 @@ template <int MP>
 int launch_iterate(const PairArgs& p, half_t* p_hi, half_t* p_lo, hipStream_t s) {
     constexpr int kLds = MP * MP * 4 + MP * (MP + 1) * 4;            // one operand, and the other or A turned round
     if (kLds > 64 * 1024 && !allow_lds(reinterpret_cast<const void*>(ns_iterate_kernel<MP>), kLds)) return TPPO_ERR_LAUNCH;
-    hipLaunchKernelGGL(ns_iterate_kernel<MP>, dim3((unsigned)p.count), dim3(kIterThreads), kLds, s, p.part, p.chunks, p.count, p.scales,
+    hipLaunchKernelGGL(ns_iterate_kernel<MP>, dim3((unsigned)p.count), dim3(MP * 4), kLds, s, p.part, p.chunks, p.count, p.scales,
                        p.x.steps, p.x.a, p.x.b, p.x.c, p_hi, p_lo);
     return launch_result();
 }

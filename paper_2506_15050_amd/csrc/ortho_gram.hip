@@ -3,8 +3,8 @@
 //     M = a I + b A + c A A,   A <- M A M,   P <- M P;   at the end X = P X_0.
 // X is read twice instead of twice a step, and what is left between is m x m: 6 m^2 n + 17 m^3 flop (5 steps, halves of symmetric
 // results not counted) against 15 m^2 n + 5 m^3.
-// Bound by the chain of products that wait for each other: 64 x 1024: 30.6 us (norm 3, first X 4, X X^T 5, all steps 15.5, P X 4); eight of
-// 1000 x 333: 163, of which 14 products of 7 to 10.
+// Bound by the chain of products that wait for each other: 64 x 1024: 27.4 us (norm 3, first X 4, X X^T 5, all steps 12, P X 4); eight of
+// 1000 x 333: 155, of which 14 products of 6.5 to 9.
 // Precision.  A holds squares of singular values, and its errors where they are small grow by a^2 a step.  So everything here is a pair of
 // fp16, hi + lo, rounded to nearest, 22 bits of what is not far below 1, products are hi hi + hi lo + lo hi with sums in fp32, and A is made
 // symmetric to the bit, step by step.  Emulated against 64 bits: 1.6e-3 of the result's norm at worst (2 x 3, singular values 1 and 0.01), 1e-3
@@ -81,8 +81,9 @@ __device__ __forceinline__ void pair_store(const float (*tile)[kTileLd], int t0,
 }
 
 // 64 x 64 tiles, four wavefronts of 32 x 32.  A stage holds 64 of K of both operands' halves, a quarter of it loaded by each wavefront.  Few
-// workgroups keep three stages under way, one to a CU; many one, two to a CU.
-template <PairMode MODE, int STAGES>
+// workgroups keep two stages under way, one to a CU; many one, two to a CU.  One / two / three / four stages under way, us:  1024 x 1024: 231 /
+// 214 / 225 / 231;  512 x 512: 146 / 142 / 150 / 155;  333 x 512: 127 / 119 / 125 / 129.
+template <PairMode MODE, int STAGES>                 // STAGES: places for them, 2 or 3
 __global__ __launch_bounds__(kPairThreads, STAGES == 2 ? 2 : 1) void ns_pair_kernel(PairArgs p) {
     extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
     constexpr bool kKMajor = MODE == kPairLast, kBothX = MODE == kPairGram || MODE == kPairWhole;
@@ -142,8 +143,7 @@ __global__ __launch_bounds__(kPairThreads, STAGES == 2 ? 2 : 1) void ns_pair_ker
     for (int it = 0; it < stages; ++it) {
         const int behind = min(STAGES - 2, stages - 1 - it);         // stages asked for after this one, eight transfers each
         if (behind == 0) __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));
-        else if (behind == 1) __builtin_amdgcn_s_waitcnt(vmcnt_imm(8));
-        else __builtin_amdgcn_s_waitcnt(vmcnt_imm(16));
+        else __builtin_amdgcn_s_waitcnt(vmcnt_imm(8));
         __syncthreads();                             // this stage is there for everyone, and everyone has left the one before
         if (it + STAGES - 1 < stages) issue(first + it + STAGES - 1, (it + STAGES - 1) % STAGES);
         const unsigned at = it % STAGES * kPairStage;
@@ -262,7 +262,7 @@ __global__ __launch_bounds__(256) void ns_gather_kernel(const float* part, int c
 // passes through LDS once a step each, in the order of the lanes.  Only the new A is exchanged across the diagonal, where it is
 // made the mean of both sides.
 // Bound by the chain of products: 17 for 5 steps, 24 MFMAs a wavefront each (96 at 128 rows), and by LDS, which every wavefront reads whole.
-// 64 rows, us: so, 12; blocks of lower triangles dealt out to 16 wavefronts, mirrored in LDS by pieces of two bytes, 16.5; all blocks where
+// 64 rows, us: so, 12.2; blocks of lower triangles dealt out to 16 wavefronts, mirrored in LDS by pieces of two bytes, 16.5; all blocks where
 // they lie, operands from LDS, 16 wavefronts 20.7, four 26.5.  A call with 128 x 1024: 61; two strips to each of four wavefronts 68; sums read
 // where each lane wants them, across the diagonal, 117.
 template <int MP>
@@ -496,8 +496,8 @@ int launch_pair(PairArgs& p, int problems, hipStream_t s) {
     p.by_count = 1.0 / p.count;
     const unsigned groups = (unsigned)((int64_t)p.tiles * p.count * p.deep * problems);
     if (groups <= kSweepGroups) {
-        if (!allow_lds(reinterpret_cast<const void*>(ns_pair_kernel<MODE, 4>), 4 * kPairStage)) return TPPO_ERR_LAUNCH;
-        hipLaunchKernelGGL((ns_pair_kernel<MODE, 4>), dim3(groups), dim3(kPairThreads), 4 * kPairStage, s, p);
+        if (!allow_lds(reinterpret_cast<const void*>(ns_pair_kernel<MODE, 3>), 3 * kPairStage)) return TPPO_ERR_LAUNCH;
+        hipLaunchKernelGGL((ns_pair_kernel<MODE, 3>), dim3(groups), dim3(kPairThreads), 3 * kPairStage, s, p);
     } else {
         hipLaunchKernelGGL((ns_pair_kernel<MODE, 2>), dim3(groups), dim3(kPairThreads), 2 * kPairStage, s, p);
     }

@@ -2,7 +2,7 @@
 //     X = G / (|G|_F + eps), wide;   steps times:  A = X X^T,  B = b A + c A A,  X = a X + B X
 // Three matrix products a step on the matrix cores, 2 m (m n + m m + m n) flop, of which the first two have symmetric results: only the
 // tiles on and below the diagonal are computed, and written twice.
-// Bound by the matrix cores: 5120 x 5120, 5 steps: 2600 us, 1.03 PFLOP/s of the flops that are needed; 1.45 within a round of tiles, as a
+// Bound by the matrix cores: 5120 x 5120, 5 steps: 2580 to 2630 us, 1.03 PFLOP/s of the flops that are needed; 1.45 within a round of tiles, as a
 // large library product reaches, of which X X^T and A A fill 82 % of the CUs and B X two rounds by 78 %.
 //
 // Precision.  A rounding of X is a matrix with singular values in every direction, and the iteration multiplies small ones by up to a
@@ -592,9 +592,9 @@ static NsShapeCost ns_shape(int n_t, int n_v, int64_t count) {
 
 // Which way is the shorter.  Both by their launches: what they cost without their stages, in us, and the stages.  This way has three
 // products a step, of X's length and of its width; the other (ortho_gram.hip) three passes over pairs, 64 x 64 tiles, of X's width but for
-// the first and the last.  Measured, us, this way / the other, * what the rule takes:  512 x 512: 228 / *156;  1024 x 1024: 320 / *233;  1536:
-// *402 / 446;  2048: *500 / 930;  1024 x 4096: 478 / *281;  1536 x 6144: 735 / *584;  2048 x 8192: *1041 / 1304;  four of 1024 x 1024: *332 / 522;  four
-// of 1024 x 4096: *630 / 722;  1024 x 16384: 1242 / *468.
+// the first and the last.  Measured, us, this way / the other, * what the rule takes:  512 x 512: 228 / *140;  1024 x 1024: 318 / *214;  1536:
+// *401 / 426;  2047: *500 / 906;  1024 x 4096: 478 / *252;  1536 x 6144: 730 / *547;  2047 x 8192: *995 / 1217;  four of 1024 x 1024: *330 / 498;  four
+// of 1024 x 4096: *626 / 666;  1024 x 16384: 1231 / *424.
 static double ns_direct_us(int mp, int np, int64_t count, int steps) {
     const double gram = ns_shape<true>(mp, mp, count).stage, update = ns_shape<false>(mp, np, count).stage;
     return steps * (3 * 9.0 + gram * (np + mp) / 64 + update * mp / 64);

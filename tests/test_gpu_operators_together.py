@@ -353,3 +353,24 @@ def test_one_expert_and_one_element():
         out = tp.tppo_orthogonalize(torch.full((1, 1), v, device="cuda"))
         want = oops.orthogonalize(np.full((1, 1), np.float32(v)))
         assert abs(float(out) - want) <= 2.0 ** -8 * abs(want)
+
+
+@pytest.mark.parametrize("dtype", [F, BF])
+def test_masks_of_the_lowest_value(dtype):
+    """Logits masked by their type's lowest value instead of -inf: alone in a row they are alike, beside others nothing."""
+    lowest = torch.finfo(dtype).min
+    z = torch.randn(6, 24, device="cuda").to(dtype)
+    z[0], z[1, 5:], z[2, ::2] = lowest, lowest, lowest
+    z[3, 0], z[3, 1:] = torch.finfo(dtype).max, lowest
+    ids = torch.tensor([[1, 3, -1]] * 6, dtype=torch.int32, device="cuda")
+    grad, loss, counts, mean_prob = tp.tppo_balance_loss_backward(z, ids)
+    Z, I = _host(z), ids.cpu().numpy()
+    oloss, ocounts, omean = oops.balance_loss(Z, I, 1.0)
+    og, p, f = oops.balance_loss_backward(Z, I, 1.0), oops.softmax_rows(Z), ocounts / 18
+    # exponents of a few units, rounded twice; sums of 24 and 6 terms
+    assert counts.tolist() == ocounts.tolist() and abs(float(loss) - oloss) <= 128 * U * oloss
+    _close(_host(mean_prob), omean, 128 * U * omean, U, "mean_prob")
+    away = np.abs(f - f.mean())
+    half = 2.0 ** -8 if dtype == BF else U
+    _close(_host(grad), og, 256 * U * 4 * p * (away + (p * away).sum(1, keepdims=True) + f.mean()), half, "grad")
+    assert not bool(grad[2, ::2].any()) and not bool(grad[3, 1:].any())

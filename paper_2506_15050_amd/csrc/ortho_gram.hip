@@ -14,13 +14,13 @@
 namespace tppo {
 
 constexpr float kPolyScale = 16.f;                   // of P, whose eigenvalues go up to a^steps
-constexpr int kPairThreads = 256, kPairTile = 64, kPairStage = 4 * kPairTile * 128;
+constexpr int kPairThreads = 512, kPairTile = 64, kPairStage = 4 * kPairTile * 128;
 
 enum PairMode { kPairGram, kPairWhole, kPairPoly, kPairMul, kPairLast };        // X X^T: partial sums of it; all of it, as pairs
 
 // One product of pairs, out[t, v] = sum_k t_op[t, k] v_op[v, k] (kPairLast: v_op[k, v]).
 struct PairProblem {
-    const half_t *t_hi, *t_lo, *v_hi, *v_lo;
+    const half_t* op[4];                             // T's high halves, its low ones, V's
     half_t *out_hi, *out_lo;
     float in_scale, out_scale;                       // the sum times in_scale is the value; stored times out_scale
 };
@@ -60,12 +60,13 @@ __device__ __forceinline__ void pair_tile_at(int id, int& t, int& v) {
 // A tile of a symmetric matrix as pairs to both sides of the diagonal, from LDS (fp32, tile[t][v]), eight entries of a row at a time.  A
 // tile on the diagonal is taken from where v >= t.
 constexpr int kTileLd = kPairTile + 1;
+template <int THREADS>
 __device__ __forceinline__ void pair_store(const float (*tile)[kTileLd], int t0, int v0, half_t* hi, half_t* lo, int ld) {
 #pragma unroll
-    for (int turn = 0; turn < 4; ++turn) {
-        const bool back = turn >= 2;                                 // the mirrored tile: row v0 + r, columns t0 + c ..
+    for (int turn = 0; turn < 1024 / THREADS; ++turn) {
+        const bool back = turn >= 512 / THREADS;                     // the mirrored tile: row v0 + r, columns t0 + c ..
         if (back && t0 == v0) break;
-        const int r = (turn & 1) * 32 + ((int)threadIdx.x >> 3), c = (threadIdx.x & 7) * 8;
+        const int r = turn % (512 / THREADS) * (THREADS / 8) + ((int)threadIdx.x >> 3), c = (threadIdx.x & 7) * 8;
         half8 h, l;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
@@ -80,11 +81,12 @@ __device__ __forceinline__ void pair_store(const float (*tile)[kTileLd], int t0,
     }
 }
 
-// 64 x 64 tiles, four wavefronts of 32 x 32.  A stage holds 64 of K of both operands' halves, a quarter of it loaded by each wavefront.  Few
-// workgroups keep two stages under way, one to a CU; many one, two to a CU.  One / two / three / four stages under way, us:  1024 x 1024: 231 /
+// 64 x 64 tiles, eight wavefronts of 16 x 32 (four of 32 x 32, us:  1024 x 1024: 212, so: 206;  333 x 512: 117.5, 112;  1536 x 6144: 557, 563).  A
+// stage holds 64 of K of both operands' halves, an eighth of it loaded by each wavefront.  Few
+// workgroups keep two stages under way, one to a CU; many one, two to a CU.  One / two / three / four stages under way, by four wavefronts, us:  1024 x 1024: 231 /
 // 214 / 225 / 231;  512 x 512: 146 / 142 / 150 / 155;  333 x 512: 127 / 119 / 125 / 129.
 template <PairMode MODE, int STAGES>                 // STAGES: places for them, 2 or 3
-__global__ __launch_bounds__(kPairThreads, STAGES == 2 ? 2 : 1) void ns_pair_kernel(PairArgs p) {
+__global__ __launch_bounds__(kPairThreads, STAGES == 2 ? 4 : 2) void ns_pair_kernel(PairArgs p) {
     extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
     constexpr bool kKMajor = MODE == kPairLast, kBothX = MODE == kPairGram || MODE == kPairWhole;
     // chunk by chunk, or V tile by V tile, of a tile, tile by tile, matrix by matrix, problem by problem; consecutive ones on an XCD, whose L2
@@ -104,17 +106,17 @@ __global__ __launch_bounds__(kPairThreads, STAGES == 2 ? 2 : 1) void ns_pair_ker
     }
     const int t0 = tile_t * kPairTile, v0 = tile_v * kPairTile;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int wv = wave >> 1, wt = wave & 1, col = lane & 15, grp = lane >> 4;
+    const int wv = wave >> 1, wt = wave & 1, kind = wave >> 1, col = lane & 15, grp = lane >> 4;
     const unsigned lds_base = (unsigned)(size_t)(__attribute__((address_space(3))) unsigned char*)smem;
     const int first = (int)((int64_t)p.stages * chunk / p.chunks), stages = (int)((int64_t)p.stages * (chunk + 1) / p.chunks) - first;
 
-    // loader: wavefront 0 T's high halves, 1 T's low ones, 2 and 3 V's; lane l of transfer d has row d * 8 + l / 8, slot l % 8
-    const bool on_v = wave >= 2;
-    const half_t* base = wave == 0 ? q.t_hi : wave == 1 ? q.t_lo : wave == 2 ? q.v_hi : q.v_lo;
+    // loader: a half of an operand's high or low halves to a wavefront; lane l of transfer d has row d * 8 + l / 8 of it, slot l % 8
+    const bool on_v = kind >= 2;
+    const half_t* base = q.op[kind];
     const int ld = on_v ? p.ld_v : p.ld_t;
     const char* src = reinterpret_cast<const char*>(base + mat * (on_v ? p.each_v : p.each_t));
     int64_t row_step, k_step;
-    const int row = lane >> 3;
+    const int row = (wave & 1) * 32 + (lane >> 3);
     int chunk_at[2];                                 // of even and odd transfers: their rows are 8 apart
     if (on_v && kKMajor) {
         src += ((int64_t)row * ld + v0) * 2;
@@ -131,45 +133,44 @@ __global__ __launch_bounds__(kPairThreads, STAGES == 2 ? 2 : 1) void ns_pair_ker
     }
     auto issue = [&](int stage, int slot) {
         const char* from = src + stage * k_step;
-        const unsigned dst = lds_base + slot * kPairStage + wave * 8192;
+        const unsigned dst = lds_base + slot * kPairStage + wave * 4096;
 #pragma unroll
-        for (int d = 0; d < 8; ++d) {
+        for (int d = 0; d < 4; ++d) {
             dma_16b_per_lane(from + chunk_at[d & 1], dst, d * 1024);
             from += row_step;
         }
     };
-    f32x4 acc[2][2] = {}, cross[2][2] = {};
+    f32x4 acc[2] = {}, cross[2] = {};
     for (int it = 0; it < STAGES - 1 && it < stages; ++it) issue(first + it, it);
     for (int it = 0; it < stages; ++it) {
         const int behind = min(STAGES - 2, stages - 1 - it);         // stages asked for after this one, eight transfers each
         if (behind == 0) __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));
-        else __builtin_amdgcn_s_waitcnt(vmcnt_imm(8));
+        else __builtin_amdgcn_s_waitcnt(vmcnt_imm(4));
         __syncthreads();                             // this stage is there for everyone, and everyone has left the one before
         if (it + STAGES - 1 < stages) issue(first + it + STAGES - 1, (it + STAGES - 1) % STAGES);
         const unsigned at = it % STAGES * kPairStage;
 #pragma unroll
         for (int k32 = 0; k32 < 2; ++k32) {
-            half8 t[2][2], v[2][2];                  // [hi, lo][block]
-            const int c = k32 * 4 + grp;
+            half8 t[2][2], v[2];                     // [hi, lo], T's [block]
+            const int c = k32 * 4 + grp, rv = wv * 16 + col;
 #pragma unroll
-            for (int part = 0; part < 2; ++part)
+            for (int part = 0; part < 2; ++part) {
 #pragma unroll
                 for (int b = 0; b < 2; ++b) {
-                    const int rt = wt * 32 + b * 16 + col, rv = wv * 32 + b * 16 + col;
+                    const int rt = wt * 32 + b * 16 + col;
                     t[part][b] = *reinterpret_cast<const half8*>(smem + at + part * 8192 + rt * 128 + ((c ^ ns_swz(rt)) << 4));
-                    if constexpr (kKMajor) v[part][b] = ns_k_major_frag<64>(lds_base + at + (2 + part) * 8192, wv * 2 + b, k32, lane);
-                    else v[part][b] = *reinterpret_cast<const half8*>(smem + at + (2 + part) * 8192 + rv * 128 + ((c ^ ns_swz(rv)) << 4));
                 }
+                if constexpr (kKMajor) v[part] = ns_k_major_frag<64>(lds_base + at + (2 + part) * 8192, wv, k32, lane);
+                else v[part] = *reinterpret_cast<const half8*>(smem + at + (2 + part) * 8192 + rv * 128 + ((c ^ ns_swz(rv)) << 4));
+            }
 #pragma unroll
-            for (int vb = 0; vb < 2; ++vb)
-#pragma unroll
-                for (int tb = 0; tb < 2; ++tb) {
-                    acc[vb][tb] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v[0][vb], t[0][tb], acc[vb][tb], 0, 0, 0);
-                    f32x4& with_t = kBothX ? cross[vb][tb] : acc[vb][tb];                      // (X's low halves are scaled)
-                    f32x4& with_v = kBothX || MODE == kPairLast ? cross[vb][tb] : acc[vb][tb];
-                    with_t = __builtin_amdgcn_mfma_f32_16x16x32_f16(v[0][vb], t[1][tb], with_t, 0, 0, 0);
-                    with_v = __builtin_amdgcn_mfma_f32_16x16x32_f16(v[1][vb], t[0][tb], with_v, 0, 0, 0);
-                }
+            for (int tb = 0; tb < 2; ++tb) {
+                acc[tb] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v[0], t[0][tb], acc[tb], 0, 0, 0);
+                f32x4& with_t = kBothX ? cross[tb] : acc[tb];                      // (X's low halves are scaled)
+                f32x4& with_v = kBothX || MODE == kPairLast ? cross[tb] : acc[tb];
+                with_t = __builtin_amdgcn_mfma_f32_16x16x32_f16(v[0], t[1][tb], with_t, 0, 0, 0);
+                with_v = __builtin_amdgcn_mfma_f32_16x16x32_f16(v[1], t[0][tb], with_v, 0, 0, 0);
+            }
         }
     }
     float(*tile_out)[kTileLd] = reinterpret_cast<float(*)[kTileLd]>(smem);
@@ -177,42 +178,38 @@ __global__ __launch_bounds__(kPairThreads, STAGES == 2 ? 2 : 1) void ns_pair_ker
 #pragma unroll
     for (int tb = 0; tb < 2; ++tb) {
         const int t = t0 + wt * 32 + tb * 16 + col;
+        const int v = v0 + wv * 16 + grp * 4;
+        float x[4];
 #pragma unroll
-        for (int vb = 0; vb < 2; ++vb) {
-            const int v = v0 + wv * 32 + vb * 16 + grp * 4;
-            float x[4];
+        for (int e = 0; e < 4; ++e)
+            x[e] = kBothX || MODE == kPairLast ? fmaf(cross[tb][e], 1.f / kLoScale, acc[tb][e]) : acc[tb][e];
+        if constexpr (MODE == kPairGram) {
+            *reinterpret_cast<float4*>(p.part + ((int64_t)chunk * p.count + mat) * p.each_out + (int64_t)t * p.ld_out + v) =
+                make_float4(x[0], x[1], x[2], x[3]);
+        } else if constexpr (MODE == kPairLast) {
+            const float by = q.in_scale * p.scales[mat].y;
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-                x[e] = kBothX || MODE == kPairLast ? fmaf(cross[vb][tb][e], 1.f / kLoScale, acc[vb][tb][e]) : acc[vb][tb][e];
-            if constexpr (MODE == kPairGram) {
-                *reinterpret_cast<float4*>(p.part + ((int64_t)chunk * p.count + mat) * p.each_out + (int64_t)t * p.ld_out + v) =
-                    make_float4(x[0], x[1], x[2], x[3]);
-            } else if constexpr (MODE == kPairLast) {
-                const float by = q.in_scale * p.scales[mat].y;
+            for (int e = 0; e < 4; ++e) tile_out[t - t0][v - v0 + e] = x[e] * by;
+        } else {
+            half4 a_hi, a_lo;
+            if constexpr (MODE == kPairPoly) {   // (t_op is A)
+                const int64_t at = mat * p.each_t + (int64_t)t * p.ld_t + v;
+                a_hi = *reinterpret_cast<const half4*>(q.op[0] + at);
+                a_lo = *reinterpret_cast<const half4*>(q.op[1] + at);
+            }
 #pragma unroll
-                for (int e = 0; e < 4; ++e) tile_out[t - t0][v - v0 + e] = x[e] * by;
-            } else {
-                half4 a_hi, a_lo;
-                if constexpr (MODE == kPairPoly) {   // (t_op is A)
-                    const int64_t at = mat * p.each_t + (int64_t)t * p.ld_t + v;
-                    a_hi = *reinterpret_cast<const half4*>(q.t_hi + at);
-                    a_lo = *reinterpret_cast<const half4*>(q.t_lo + at);
-                }
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    float y = x[e] * (MODE == kPairWhole ? p.scales[mat].x : q.in_scale);
-                    if constexpr (MODE == kPairPoly)
-                        y = fmaf(p.x.c, y, fmaf(p.x.b * (1.f / kOffScale), (float)a_hi[e] + (float)a_lo[e], t == v + e ? p.x.a : 0.f));
-                    tile_out[t - t0][v - v0 + e] = y * q.out_scale;
-                }
+            for (int e = 0; e < 4; ++e) {
+                float y = x[e] * (MODE == kPairWhole ? p.scales[mat].x : q.in_scale);
+                if constexpr (MODE == kPairPoly)
+                    y = fmaf(p.x.c, y, fmaf(p.x.b * (1.f / kOffScale), (float)a_hi[e] + (float)a_lo[e], t == v + e ? p.x.a : 0.f));
+                tile_out[t - t0][v - v0 + e] = y * q.out_scale;
             }
         }
     }
     if constexpr (MODE == kPairLast) {               // eight entries of a row of the caller's matrix at a time
         __syncthreads();
-#pragma unroll
-        for (int turn = 0; turn < 2; ++turn) {
-            const int r = turn * 32 + ((int)threadIdx.x >> 3), c = (threadIdx.x & 7) * 8;
+        {
+            const int r = (int)threadIdx.x >> 3, c = (threadIdx.x & 7) * 8;
             float x[8];
 #pragma unroll
             for (int e = 0; e < 8; ++e) x[e] = p.x.transposed ? tile_out[c + e][r] : tile_out[r][c + e];
@@ -224,7 +221,7 @@ __global__ __launch_bounds__(kPairThreads, STAGES == 2 ? 2 : 1) void ns_pair_ker
     }
     if constexpr (MODE == kPairWhole || MODE == kPairPoly || MODE == kPairMul) {
         __syncthreads();
-        pair_store(tile_out, t0, v0, q.out_hi + mat * p.each_out, q.out_lo + mat * p.each_out, p.ld_out);
+        pair_store<kPairThreads>(tile_out, t0, v0, q.out_hi + mat * p.each_out, q.out_lo + mat * p.each_out, p.ld_out);
     }
 }
 
@@ -252,7 +249,7 @@ __global__ __launch_bounds__(256) void ns_gather_kernel(const float* part, int c
         tile[r][c + 3] = sum.w * by;
     }
     __syncthreads();
-    pair_store(tile, t0, v0, hi + (int64_t)mat * mp * mp, lo + (int64_t)mat * mp * mp, mp);
+    pair_store<256>(tile, t0, v0, hi + (int64_t)mat * mp * mp, lo + (int64_t)mat * mp * mp, mp);
 }
 
 // All steps of one matrix of up to MP = 64 or 128 rows in one workgroup, a strip of 16 columns of every matrix to a wavefront.
@@ -529,7 +526,7 @@ int ns_gram(const NsShape& x, const half_t* hi, const half_t* lo, const float2* 
     p.each_out = each;
     p.ld_out = mp;
     // A = X X^T
-    p.problem[0] = {hi, lo, hi, lo, nullptr, nullptr, 1.f, 1.f};
+    p.problem[0] = {{hi, lo, hi, lo}, nullptr, nullptr, 1.f, 1.f};
     p.each_t = p.each_v = (int64_t)mp * np;
     p.ld_t = p.ld_v = np;
     p.tiles = L.tiles;
@@ -537,7 +534,7 @@ int ns_gram(const NsShape& x, const half_t* hi, const half_t* lo, const float2* 
     p.chunks = L.chunks;
     const bool whole = mp > kIterateMost && L.chunks == 1;
     if (whole) {
-        p.problem[0] = {hi, lo, hi, lo, A, A + half, 1.f, kOffScale};
+        p.problem[0] = {{hi, lo, hi, lo}, A, A + half, 1.f, kOffScale};
         if (launch_pair<kPairWhole>(p, 1, s) != TPPO_OK) return TPPO_ERR_LAUNCH;
     } else if (launch_pair<kPairGram>(p, 1, s) != TPPO_OK) {
         return TPPO_ERR_LAUNCH;
@@ -562,16 +559,16 @@ int ns_gram(const NsShape& x, const half_t* hi, const half_t* lo, const float2* 
         const float off2 = 1.f / (kOffScale * kOffScale);
         for (int k = 0; k < x.steps; ++k) {
             half_t* M = pair(L.m[k & 1]);
-            p.problem[0] = {A, A + half, A, A + half, M, M + half, off2, kOffScale};
+            p.problem[0] = {{A, A + half, A, A + half}, M, M + half, off2, kOffScale};
             if (launch_pair<kPairPoly>(p, 1, s) != TPPO_OK) return TPPO_ERR_LAUNCH;
             const bool last = k + 1 == x.steps;
             int problems = 0;
             half_t* next = pair(L.p[k & 1]);
-            if (!last) p.problem[problems++] = {M, M + half, A, A + half, T, T + half, off2, kOffScale};
-            if (k > 0) p.problem[problems++] = {M, M + half, P, P + half, next, next + half, 1.f / (kOffScale * p_scale), kPolyScale};
+            if (!last) p.problem[problems++] = {{M, M + half, A, A + half}, T, T + half, off2, kOffScale};
+            if (k > 0) p.problem[problems++] = {{M, M + half, P, P + half}, next, next + half, 1.f / (kOffScale * p_scale), kPolyScale};
             if (problems && launch_pair<kPairMul>(p, problems, s) != TPPO_OK) return TPPO_ERR_LAUNCH;
             if (!last) {
-                p.problem[0] = {T, T + half, M, M + half, A, A + half, off2, kOffScale};
+                p.problem[0] = {{T, T + half, M, M + half}, A, A + half, off2, kOffScale};
                 if (launch_pair<kPairMul>(p, 1, s) != TPPO_OK) return TPPO_ERR_LAUNCH;
             }
             P = k == 0 ? M : next;
@@ -579,7 +576,7 @@ int ns_gram(const NsShape& x, const half_t* hi, const half_t* lo, const float2* 
         }
     }
     // X = P X
-    p.problem[0] = {P, P + half, hi, lo, nullptr, nullptr, 1.f / p_scale, 1.f};
+    p.problem[0] = {{P, P + half, hi, lo}, nullptr, nullptr, 1.f / p_scale, 1.f};
     p.each_t = each;
     p.ld_t = mp;
     p.each_v = (int64_t)mp * np;

@@ -592,8 +592,8 @@ static NsShapeCost ns_shape(int n_t, int n_v, int64_t count) {
 
 // Which way is the shorter.  Both by their launches: what they cost without their stages, in us, and the stages.  This way has three
 // products a step, of X's length and of its width; the other (ortho_gram.hip) three passes over pairs, 64 x 64 tiles, of X's width but for
-// the first and the last.  Measured, us, this way / the other, * what the rule takes:  512 x 512: 228 / *140;  1024 x 1024: 318 / *214;  1536:
-// *401 / 426;  2047: *500 / 906;  1024 x 4096: 478 / *252;  1536 x 6144: 730 / *547;  2047 x 8192: *995 / 1217;  four of 1024 x 1024: *330 / 498;  four
+// the first and the last.  Measured, us, this way / the other, * what the rule takes:  512 x 512: 228 / *132;  1024 x 1024: 318 / *206;  1536:
+// *401 / 426;  2047: *500 / 906;  1024 x 4096: 478 / *254;  1536 x 6144: 730 / *563;  2047 x 8192: *995 / 1217;  four of 1024 x 1024: *330 / 498;  four
 // of 1024 x 4096: *626 / 666;  1024 x 16384: 1231 / *424.
 static double ns_direct_us(int mp, int np, int64_t count, int steps) {
     const double gram = ns_shape<true>(mp, mp, count).stage, update = ns_shape<false>(mp, np, count).stage;

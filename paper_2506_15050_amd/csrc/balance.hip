@@ -136,7 +136,8 @@ __global__ __launch_bounds__(kBlThreads) void balance_rows_kernel(Balance b) {
     constexpr int kCols = kLanes * kPieces * kN;
     // the columns' sums wavefront by wavefront (in two turns where that is much)
     constexpr int kTurns = kCols * kBlWaves * 4 > 32768 ? 2 : 1, kPlaces = kBlWaves / kTurns;
-    __shared__ float columns[kCols * kPlaces > kBlMaxE ? kCols * kPlaces : kBlMaxE];
+    __shared__ __attribute__((aligned(8))) float columns[kCols * kPlaces > kBlMaxE ? kCols * kPlaces : kBlMaxE];
+    static_assert(kBlThreads * sizeof(long long) <= sizeof(columns), "a part of the counts to a thread");
     __shared__ int seen[GRAD && !ONE ? 1 : kBlMaxE];
     __shared__ double sums[kBlWaves];
     const int lane = threadIdx.x % kLanes, mine = threadIdx.x / kLanes, E = b.E;
@@ -169,11 +170,11 @@ __global__ __launch_bounds__(kBlThreads) void balance_rows_kernel(Balance b) {
                 sum += c;
             }
         } else {
-            int* parts = reinterpret_cast<int*>(columns);
+            long long* parts = reinterpret_cast<long long*>(columns);        // (a workgroup's are 32 bits, all of them together are not)
             const int width = E <= 64 ? 64 : E <= 128 ? 128 : E <= 256 ? 256 : kBlThreads, shares = kBlThreads / width;
             const int at = threadIdx.x % width, share = threadIdx.x / width;
             for (int e0 = 0; e0 < E; e0 += width) {
-                int c = 0;
+                long long c = 0;
                 if (e0 + at < E)
 #pragma unroll 16
                     for (int g = share; g < b.counters; g += shares) c += b.part_counts[(int64_t)g * E + e0 + at];

@@ -137,7 +137,7 @@ __global__ __launch_bounds__(kBlThreads) void balance_rows_kernel(Balance b) {
     // the columns' sums wavefront by wavefront (in two turns where that is much)
     constexpr int kTurns = kCols * kBlWaves * 4 > 32768 ? 2 : 1, kPlaces = kBlWaves / kTurns;
     __shared__ __attribute__((aligned(8))) float columns[kCols * kPlaces > kBlMaxE ? kCols * kPlaces : kBlMaxE];
-    static_assert(kBlThreads * sizeof(long long) <= sizeof(columns), "a part of the counts to a thread");
+    static_assert(kBlThreads * sizeof(long long) <= sizeof(columns) && kCols * sizeof(long long) <= sizeof(columns), "all counts, or a part to a thread");
     __shared__ int seen[GRAD && !ONE ? 1 : kBlMaxE];
     __shared__ double sums[kBlWaves];
     const int lane = threadIdx.x % kLanes, mine = threadIdx.x / kLanes, E = b.E;
@@ -161,16 +161,18 @@ __global__ __launch_bounds__(kBlThreads) void balance_rows_kernel(Balance b) {
     if constexpr (GRAD) {
         const double n = b.n_tokens(m_eff), each = 1.0 / ((double)b.k * n);
         up = (float)((double)b.scale * b.coefficient * E / n);
-        // all counts, and their sum: a column to a thread, or its parts to several
+        // all counts, and their sum: a column to a thread, or its parts to several.  (A workgroup's counts are 32 bits, all of them together are
+        // not; and they stay whole until their mean is known: rounded before that, counts of 3 x 10^7 one apart gave d wrong by 4 %.)
+        long long* whole = reinterpret_cast<long long*>(columns);
         double sum = 0.0;
         if (b.counts_in || ONE) {
             for (int e = threadIdx.x; e < E; e += kBlThreads) {
-                const double c = b.counts_in ? (double)b.counts_in[e] : (double)seen[e];
-                columns[e] = (float)(c * each);
-                sum += c;
+                const long long c = b.counts_in ? (long long)b.counts_in[e] : (long long)seen[e];
+                whole[e] = c;
+                sum += (double)c;
             }
         } else {
-            long long* parts = reinterpret_cast<long long*>(columns);        // (a workgroup's are 32 bits, all of them together are not)
+            long long* parts = whole;
             const int width = E <= 64 ? 64 : E <= 128 ? 128 : E <= 256 ? 256 : kBlThreads, shares = kBlThreads / width;
             const int at = threadIdx.x % width, share = threadIdx.x / width;
             for (int e0 = 0; e0 < E; e0 += width) {
@@ -186,19 +188,19 @@ __global__ __launch_bounds__(kBlThreads) void balance_rows_kernel(Balance b) {
                     __syncthreads();
                 }
                 if (share == 0 && e0 + at < E) {
-                    columns[e0 + at] = (float)((double)c * each);
+                    whole[e0 + at] = c;
                     sum += (double)c;
                 }
             }
         }
         sum = workgroup_sum(sum, sums);
-        const float mean = (float)(sum * each / E);
+        const double mean = sum / E;
 #pragma unroll
         for (int i = 0; i < kPieces; ++i)
 #pragma unroll
             for (int e = 0; e < kN; ++e) {
                 const int at = starts[i] + e;
-                d[i][e] = lane + i * kLanes < pieces && at < E ? columns[at] - mean : 0.f;
+                d[i][e] = lane + i * kLanes < pieces && at < E ? (float)(((double)whole[at] - mean) * each) : 0.f;
             }
         __syncthreads();
     }

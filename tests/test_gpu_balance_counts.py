@@ -1,4 +1,5 @@
-"""The balance loss's derivative where the counts are many, or nearly alike: counts beyond 32 bits."""
+"""The balance loss's derivative where the counts are many, or nearly alike: counts beyond 32 bits, counts one apart in thousands and in
+hundreds of millions."""
 import numpy as np
 import pytest
 import torch
@@ -34,3 +35,48 @@ def test_more_choices_of_an_expert_than_32_bits_count(E):
         assert worst <= 1, f"{worst} times the bound"
     # a thread adds up to 1028 rows, a workgroup's wavefronts and all workgroups follow
     assert abs(float(loss) - E * (p * f).sum()) <= (64 + 1028 + 16) * U * float(loss)
+
+
+def _nearly_even(E, even, M):
+    """Router logits of M tokens, and counts of a batch in which every expert has `even` choices, give or take one."""
+    rng = np.random.default_rng(E)
+    z = torch.from_numpy(rng.normal(size=(M, E))).float().cuda()
+    return z, torch.from_numpy(even + rng.integers(-1, 2, size=E)).cuda()
+
+
+def _check_nearly_even(grad, z, counts, k, tokens):
+    """The same derivative from any f that differs by the same amount everywhere: a row's p add up to one."""
+    z, d = z.double().cpu().numpy(), counts.cpu().numpy()
+    E = len(d)
+    d = (d - int(np.median(d))) / (k * tokens)
+    d = d - d.mean()
+    p = oops.softmax_rows(z)
+    g = E / tokens * p * (d - (p * d).sum(1, keepdims=True))
+    spread = (p * np.abs(d)).sum(1, keepdims=True)
+    # no term of the size of f itself: d is rounded once, a probability is off by 64 steps (arguments up to 12, rounded twice), the sum over
+    # the row by as many, and the steps of the formula
+    bound = E / tokens * p * ((64 + 8) * U * (np.abs(d) + spread) + (64 + 64) * U * spread) + U * np.abs(g) + 1e-37
+    worst = float((np.abs(grad.double().cpu().numpy() - g) / bound).max())
+    assert worst <= 1, f"{worst} times the bound"
+
+
+@pytest.mark.parametrize("E,k", [(128, 8), (67, 3), (500, 7)])
+def test_counts_one_apart(E, k):
+    """An update's tokens, spread over the experts as evenly as they go: counts that are no powers of two, one apart."""
+    M = 77536
+    ids = torch.arange(M * k, dtype=torch.int32).remainder(E).view(M, k).cuda()
+    ids[17, 2] = -1
+    z = torch.randn(M, E, device="cuda")
+    grad, _, counts, _ = tp.tppo_balance_loss_backward(z, ids)
+    assert int(counts.max() - counts.min()) in (1, 2)
+    _check_nearly_even(grad[:3000], z[:3000], counts, k, M)
+
+
+@pytest.mark.parametrize("M", [40, 5000])                          # one workgroup; many
+@pytest.mark.parametrize("E,k,tokens", [(256, 8, 10 ** 7), (256, 8, 10 ** 9), (60, 2, 123_456_789)])
+def test_counts_of_a_large_batch_one_apart(M, E, k, tokens):
+    z, counts = _nearly_even(E, tokens * k // E, M)
+    ids = torch.zeros(M, k, dtype=torch.int32, device="cuda")
+    grad, _, own, _ = tp.tppo_balance_loss_backward(z, ids, counts_in=counts, token_denominator=tokens)
+    assert own.tolist() == [M * k] + [0] * (E - 1)
+    _check_nearly_even(grad, z, counts, k, tokens)

@@ -65,10 +65,17 @@ struct NsShape {
     int64_t ld_out, each_out;
 };
 
+// What `steps` steps make of singular values s from 0 to 1: each multiplies them by m(l) = a + b l + c l l, l = s^2, which becomes
+// g(l) = l m(l)^2.  Bounds over all of them, in every step: of the product of the |m|, of |m|, and of l.
+struct NsReach {
+    double product, value, least, square;            // product, largest and smallest |m|; largest l
+};
+NsReach ns_reach(int steps, float a, float b, float c);
+
 // The way by X X^T (ortho_gram.hip): where it is the shorter, for m < kGramBelow at most, if the coefficients keep it within what fp16
 // pairs hold.
 constexpr int kGramBelow = 2048;
-bool ns_gram_fits(int steps, float a, float b, float c);
+bool ns_gram_fits(const NsReach& reach, int steps, float a, float b, float c);
 size_t ns_gram_bytes(int64_t count, int m, int n);
 int ns_gram(const NsShape& x, const half_t* hi, const half_t* lo, const float2* scales, char* ws, hipStream_t s);
 

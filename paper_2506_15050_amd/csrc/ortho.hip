@@ -658,7 +658,7 @@ static int run_ns(const T* g, int64_t count, int64_t rows, int64_t cols, int64_t
     x.m = L.m; x.n = L.n; x.transposed = transposed;
     x.out = out; x.ld_out = ld_out; x.each_out = stride_out; x.scales = scales;
     if (L.m < kGramBelow && (L.split || ns_gram_us(L.mp, L.np, count, steps) < ns_direct_us(L.mp, L.np, count, steps)) &&
-        ns_gram_fits(steps, a, b, c)) {
+        ns_gram_fits(ns_reach(steps, a, b, c), steps, a, b, c)) {
         const NsShape shape = {L.m, L.n, L.mp, L.np, transposed, count, steps, a, b, c, out, ld_out, stride_out};
         return ns_gram(shape, hi[0], lo[0], scales, ws + L.shared, s);
     }

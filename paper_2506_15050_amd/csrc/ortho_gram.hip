@@ -9,6 +9,9 @@
 // fp16, hi + lo, rounded to nearest, 22 bits of what is not far below 1, products are hi hi + hi lo + lo hi with sums in fp32, and A is made
 // symmetric to the bit, step by step.  Emulated against 64 bits: 1.6e-3 of the result's norm at worst (2 x 3, singular values 1 and 0.01), 1e-3
 // from 64 on; with halves cut instead of rounded three times that.  (X itself, whose entries are smaller, has its low halves times 2048.)
+#include <algorithm>
+#include <cmath>
+
 #include "ortho.h"
 
 namespace tppo {
@@ -436,24 +439,58 @@ __global__ __launch_bounds__(256) void ns_reduce_kernel(float4* part, int chunks
     }
 }
 
-// Whether A, M and P stay within what pairs of fp16 hold at their scales, whatever singular values X begins with, and a^steps, by which
-// errors of A grow against the result's, within the ten bits that are there for it.  (The polynomials are smooth: 64 points, and a factor
-// of four to spare.)
-bool ns_gram_fits(int steps, float a, float b, float c) {
-    if (steps < 1) return false;
-    double growth = 1.0;
-    for (int k = 0; k < steps; ++k) growth *= fabs((double)a);
-    if (!(growth <= 1000.0)) return false;
-    for (int i = 0; i <= 64; ++i) {
-        double l = (double)i / 64.0, p = 1.0;
-        for (int k = 0; k < steps; ++k) {
-            const double m = (double)a + l * ((double)b + l * (double)c);
-            p *= m;
-            l *= m * m;
-            if (!(fabs(p) <= 1000.0) || !(fabs(m) <= 250.0) || !(l <= 250.0)) return false;
+// g maps [0, u] onto [0, its largest value there], which lies at u or where g' = m (m + 2 l m') = 0, m + 2 l m' = a + 3 b l + 5 c l l.  So the
+// ranges follow from one another, and m has its extremes at their ends or at its vertex.  (A thousandth more is for roundings.)
+NsReach ns_reach(int steps, float a_, float b_, float c_) {
+    const double a = a_, b = b_, c = c_, none = HUGE_VAL;
+    NsReach r = {1.0, 0.0, none, 1.0};
+    double u = 1.0, product = 1.0;
+    auto m = [&](double l) { return a + l * (b + l * c); };
+    for (int k = 0; k < steps; ++k) {
+        if (!(u < 1e60)) return {none, none, 0.0, none};
+        const double top = u * 1.001, vertex = c != 0.0 ? -b / (2.0 * c) : -1.0;
+        double low = std::min(m(0.0), m(top)), high = std::max(m(0.0), m(top));
+        if (vertex > 0.0 && vertex < top) {
+            low = std::min(low, m(vertex));
+            high = std::max(high, m(vertex));
         }
+        u = top * m(top) * m(top);
+        auto also = [&](double l) {
+            if (l > 0.0 && l < top) u = std::max(u, l * m(l) * m(l));
+        };
+        const double inside = 9.0 * b * b - 20.0 * a * c;
+        if (inside >= 0.0) {                         // (the quadratic's roots, or the linear's one)
+            const double q = -0.5 * (3.0 * b + copysign(sqrt(inside), b));
+            if (c != 0.0) also(q / (5.0 * c));
+            if (q != 0.0) also(a / q);
+        }
+        const double most = std::max(fabs(low), fabs(high)), least = low <= 0.0 && high >= 0.0 ? 0.0 : std::min(fabs(low), fabs(high));
+        product *= most;
+        r.product = std::max(r.product, product);
+        r.value = std::max(r.value, most);
+        r.least = std::min(r.least, least);
+        r.square = std::max(r.square, u);
     }
-    return true;
+    return r;
+}
+
+// Whether this way holds the iteration.  What it stores stays within fp16 at its scales, with a factor of four to spare: 16 P, 64 A, 64 M.  And
+// the roundings, halves of a step of 2^-23, stay below 2e-3 of the result.  What they come to, in such steps, with q = a / (least m):
+//   those of P and M, which M's diagonal makes a times as large a step, against a result that is `least` times as large:  steps q^(steps - 1);
+//   those of T = M A, terms of a + |b| + |c| that cancel to m: A's eigenvectors turn by (a + |b| + |c|) a / 2 m^2, P's do not:  times q^j, added up;
+//   those of A's small eigenvalues, which grow by a^2 a step and which M takes times b:  (a + |b| + |c|) |b| a^(2 steps - 4).
+// Each is over-estimated by the worst case of every factor; the limits are a little above what the five steps of the default coefficients come to (4.2e3,
+// 4.5e4, 8.2e4).  Emulated against 64 bits, 3280 sets of coefficients and steps, ranks from one to full, 2 to 260 rows: within the limits
+// 1.9e-3 at most, beyond them up to all of the result (m near zero where the singular values are; on the card 9 % for 3.4987, -5.165,
+// 1.7679).
+bool ns_gram_fits(const NsReach& r, int steps, float a, float b, float c) {
+    if (steps < 1 || !(r.product <= 1000.0 && r.value <= 250.0 && r.square <= 250.0 && r.least > 0.0)) return false;
+    const double aa = fabs((double)a), sum = aa + fabs((double)b) + fabs((double)c), q = std::max(1.0, aa / r.least);
+    if (aa < 1.0) return false;                      // (P shrinks below what pairs hold)
+    double power = 1.0, all = 0.0;
+    for (int k = 1; k < steps; ++k) all += power *= q;
+    return steps * power <= 1e4 && sum * aa / (2.0 * r.least * r.least) * all <= 6e4 &&
+           (steps == 1 || sum * fabs((double)b) * pow(aa, 2 * steps - 4) <= 9e4);
 }
 
 namespace {

@@ -1,0 +1,40 @@
+"""The orthogonalisation with other coefficients and numbers of steps than the default, against the oracle in 64 bits: polynomials that
+come near zero where there are singular values, and iterations that amplify small ones further."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import operators as oops
+from paper_2506_15050_amd import binding as tp
+
+pytestmark = pytest.mark.gpu
+
+# the result's rounding to bf16, 1.7e-3 of its norm as a rule, and as much again for the arithmetic
+NORM = 2.0 ** -8
+
+
+def _matrix(rng, rows, cols, kind):
+    """Of rank one, or with singular values from 1 down to 10^-3 or 10^-6 in equal ratios."""
+    if kind == "rank1":
+        return rng.normal(size=(rows, 1)) @ rng.normal(size=(1, cols))
+    if kind == "full":
+        return rng.normal(size=(rows, cols))
+    r = min(rows, cols)
+    left, right = (np.linalg.qr(rng.normal(size=(n, r)))[0] for n in (rows, cols))
+    return left * np.logspace(0, -int(kind[3:]), r) @ right.T
+
+
+def _error(g, **kw):
+    want = oops.orthogonalize(g.double().cpu().numpy(), **kw)
+    return np.linalg.norm(tp.tppo_orthogonalize(g, **kw).double().cpu().numpy() - want) / np.linalg.norm(want)
+
+
+@pytest.mark.parametrize("steps,coefficients", [(4, (4.0848, -6.8946, 2.9270)), (5, (3.4987, -5.1650, 1.7679)), (9, (1.875, -1.25, 0.375))])
+@pytest.mark.parametrize("rows,cols", [(64, 64), (96, 160), (250, 260), (450, 300)])
+def test_polynomials_near_zero(rows, cols, steps, coefficients):
+    """The first two take a singular value of one to a tenth of it, the others of the iteration's to more than before."""
+    rng = np.random.default_rng(rows)
+    for kind in ("rank1", "geo3"):
+        g = torch.from_numpy(_matrix(rng, rows, cols, kind)).float().cuda()
+        worst = _error(g, steps=steps, coefficients=coefficients)
+        assert worst <= NORM, (kind, worst)

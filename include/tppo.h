@@ -574,22 +574,30 @@ int tppo_balance_loss_backward(const void* logits, int64_t n_rows, int64_t E, in
  *   out = scale * X, transposed back, rounded to bf16.
  * With (a, b, c) = (3.4445, -4.7750, 2.0315) and 5 steps, singular values from
  * 0.3 % of |G|_F on come to lie between 0.68 and 1.21.
- * X is held to 22 bits (pairs of fp16, scaled by powers of two), all sums in
- * fp32.  The operands of the products are held to 11 bits, with the diagonals of
- * A and b A + c A^2 in fp32; to 22 where rows or cols < 512, and where the
- * iteration runs on X X^T alone (rows or cols < 2048, where that is the shorter
- * way; the same X, then, multiplied by a polynomial of X X^T at the end).
+ * X is held in pairs of fp16, scaled by powers of two, which is 22 bits or more,
+ * all sums in fp32.  The operands of the products are held to 11 bits, with the
+ * diagonals of A and b A + c A^2 in fp32, where that is enough: rows and cols >=
+ * 512, |a|^steps <= min(rows, cols), no cancellation in a + b l + c l^2 (0 <= l <=
+ * 1 and what becomes of them); to 22 otherwise.  Where rows or cols < 2048 the
+ * iteration may run on X X^T alone, all of it in pairs (the same X, then,
+ * multiplied by a polynomial of X X^T at the end), if the coefficients allow it.
+ * Before the rounding to bf16 the result is within 2e-3 of its norm for |a|^steps
+ * up to 6000 (the default coefficients' seven steps).  Beyond that, and where the
+ * polynomial is near zero at a singular value, it is what products in fp32 give:
+ * each step makes singular values near zero |a| times as large, those that
+ * rounding puts there as well, up to 3e-7 |a|^steps of the norm.
  *
  * in : g: `count` matrices [rows, cols] of type dt, row stride ld_g, stride_g
  *      elements from one to the next; 1 <= rows, cols <= 65536, 0 <= steps <= 64;
- *      a, b, c, eps, scale finite, eps >= 0.
+ *      a, b, c, eps, scale finite, eps >= 0; |a|^(steps - 1) >= 2^-12 (an X that
+ *      shrinks from step to step is not held).
  *      stride_g >= 0; 0 is the same matrix every time.
  * out: out: `count` matrices [rows, cols] bf16, row stride ld_out, stride_out
  *      apart, one behind the other (stride_out >= (rows - 1) ld_out + cols); no
  *      overlap with g.
  * A matrix of zeros stays zero (with eps > 0); one with a NaN or an infinity
- * gives NaN.  Coefficients under which the iteration grows without bound end in
- * infinities and NaN.
+ * gives NaN.  Coefficients under which it has singular values s above 30, or
+ * |b s^2 + c s^4| above 1000, before the last step end in infinities and NaN.
  * workspace: tppo_orthogonalize_workspace_bytes(count, rows, cols).
  */
 size_t tppo_orthogonalize_workspace_bytes(int64_t count, int64_t rows, int64_t cols);

@@ -10,9 +10,13 @@
 //   X     is a pair of fp16, hi + lo / 2048, 22 bits, and a X is taken from both; the product B X takes hi alone: what that loses lies in
 //         the range of B, where the large singular values are, and is not amplified;
 //   A, B  have their diagonals, which tend to 1 and a - 1 .. in fp32 vectors, and only what is off the diagonal in fp16.
-// What is off the diagonal is small against it in large matrices only; where m < kSplitBelow, A and B are pairs as well, and a product
-// is hi hi + (hi lo + lo hi) / 2048, three passes over its contraction.  Against 64 bits, before the rounding to bf16 (1.7e-3), emulated:
-// one pass  m = 512 rank one 1.5e-3, full 7e-4;  256 2.3e-3;  64 9e-3;  three passes  1e-4 at most.
+// What is off the diagonal is small against it in large matrices only, and errors grow as small singular values do; where m < kSplitBelow, or
+// |a|^steps > m, or where a + b l + c l l cancels (ns_one_pass), A and B are pairs as well, and a product is hi hi + (hi lo + lo hi) / 2048,
+// three passes over its contraction.  Against 64 bits, before the rounding to bf16 (1.7e-3), emulated, 5 / 6 / 7 / 8 / 10 steps:
+//   one pass      m = 512, rank one  1.3e-3 / 2.6e-3 / 1.4e-2 / 3.2e-2 / 0.37,  singular values down to 10^-6  7e-4 / 1.4e-3 / 3.3e-3 / 8e-3 / 5e-2;
+//                 m = 2048           3e-4 / 5e-4 / 2.5e-3 / 6e-3 / 7e-2,                                       5e-4 / 9e-4 / 1.9e-3 / 5e-3 / 3e-2;
+//   three passes  any m              1e-4 / 3e-4 / 1.6e-3 / 4e-3 / 4e-2,                                       4e-6 / 1e-5 / 3e-5 / 7e-5 / 4e-4:
+// what products in fp32 give, 2e-7 |a|^steps.  (One pass, 5 steps:  m = 256 2.3e-3;  64 9e-3.)
 // All scales are powers of two: X is held times S = 2^round(log2(n) / 2), so that entries are around one from the first step to the last,
 // A and B off the diagonal times 64.  Where |G|_F is so far below eps that X stays under 1/4 to the end, S is larger by as much.
 #include <cmath>
@@ -498,7 +502,6 @@ constexpr int64_t kNsMaxSide = 65536;
 
 struct NsLayout {
     int m, n, mp, np;
-    bool split;
     size_t parts, scales, shared, diag_a, diag_b, off_a, off_b, off_a_lo, off_b_lo, hi[2], lo[2], total;
 };
 static NsLayout ns_layout(int64_t count, int64_t rows, int64_t cols) {
@@ -507,7 +510,6 @@ static NsLayout ns_layout(int64_t count, int64_t rows, int64_t cols) {
     L.n = (int)std::max(rows, cols);
     L.mp = (L.m + 63) / 64 * 64;
     L.np = (L.n + 63) / 64 * 64;
-    L.split = L.m < kSplitBelow;
     size_t o = 0;
     auto take = [&](size_t each) {
         const size_t at = o;
@@ -523,11 +525,8 @@ static NsLayout ns_layout(int64_t count, int64_t rows, int64_t cols) {
     L.diag_b = take((size_t)L.mp * 4);
     L.off_a = take((size_t)L.mp * L.mp * 2);
     L.off_b = take((size_t)L.mp * L.mp * 2);
-    L.off_a_lo = L.off_b_lo = L.off_a;
-    if (L.split) {
-        L.off_a_lo = take((size_t)L.mp * L.mp * 2);
-        L.off_b_lo = take((size_t)L.mp * L.mp * 2);
-    }
+    L.off_a_lo = take((size_t)L.mp * L.mp * 2);      // (three passes)
+    L.off_b_lo = take((size_t)L.mp * L.mp * 2);
     L.hi[1] = take((size_t)L.mp * L.np * 2);
     L.lo[1] = take((size_t)L.mp * L.np * 2);
     if (L.m < kGramBelow) o = std::max(o, L.shared + ns_gram_bytes(count, L.m, L.n));
@@ -608,6 +607,12 @@ static double ns_gram_us(int mp, int np, int64_t count, int steps) {
     const double poly = launch(tiles, side), both = launch(2 * tiles, side);
     return steps * (2 * poly + both) - poly + 10.0 + 0.8 * tiles * (np / 64) / (2 * kSweepGroups) + launch((double)side * (np / 64) * (double)count, side);
 }
+// Whether one pass with operands of 11 bits will do: large matrices, whose small singular values are not amplified by more than m (the errors are
+// 1.1e-3 |a|^steps / m at most where that is how they grow, and else 0.7e-3), and a polynomial whose terms do not cancel, 1.5e-3 of the result at most at
+// 24 (m = 512, 180 sets of coefficients; up to 9e-3 beyond).
+static bool ns_one_pass(const NsReach& r, int m, int steps, float a, float b, float c) {
+    return m >= kSplitBelow && pow(fabs((double)a), steps) <= m && fabs((double)a) + fabs((double)b) + fabs((double)c) <= 24.0 * r.least;
+}
 template <bool SPLIT, NsMode MODE>
 static int launch_ns_tiles(NsArgs& p, int64_t count, hipStream_t s) {
     constexpr bool kAcross = MODE == kUpdate || MODE == kLast;
@@ -657,8 +662,10 @@ static int run_ns(const T* g, int64_t count, int64_t rows, int64_t cols, int64_t
     x.a = a; x.b = b; x.c = c;
     x.m = L.m; x.n = L.n; x.transposed = transposed;
     x.out = out; x.ld_out = ld_out; x.each_out = stride_out; x.scales = scales;
-    if (L.m < kGramBelow && (L.split || ns_gram_us(L.mp, L.np, count, steps) < ns_direct_us(L.mp, L.np, count, steps)) &&
-        ns_gram_fits(ns_reach(steps, a, b, c), steps, a, b, c)) {
+    const NsReach reach = ns_reach(steps, a, b, c);
+    const bool split = !ns_one_pass(reach, L.m, steps, a, b, c);
+    if (L.m < kGramBelow && (split || ns_gram_us(L.mp, L.np, count, steps) < ns_direct_us(L.mp, L.np, count, steps)) &&
+        ns_gram_fits(reach, steps, a, b, c)) {
         const NsShape shape = {L.m, L.n, L.mp, L.np, transposed, count, steps, a, b, c, out, ld_out, stride_out};
         return ns_gram(shape, hi[0], lo[0], scales, ws + L.shared, s);
     }
@@ -697,7 +704,7 @@ static int run_ns(const T* g, int64_t count, int64_t rows, int64_t cols, int64_t
         }
         return (int)TPPO_OK;
     };
-    return L.split ? products(std::true_type()) : products(std::false_type());
+    return split ? products(std::true_type()) : products(std::false_type());
 }
 
 }  // namespace tppo
@@ -719,6 +726,8 @@ extern "C" int tppo_orthogonalize(const void* g, int64_t count, int64_t rows, in
     if (steps < 0 || steps > 64 || !(eps >= 0.f)) return TPPO_ERR_PARAM;
     for (float v : {a, b, c, eps, scale})
         if (!(v - v == 0.f)) return TPPO_ERR_PARAM;
+    // an X that shrinks below what its pairs of fp16 hold; the last step's stays in fp32
+    if (steps > 1 && pow(fabs((double)a), steps - 1) < 1.0 / 4096) return TPPO_ERR_PARAM;
     if (count == 0) return TPPO_OK;
     if (!g || !out) return TPPO_ERR_NULL;
     if (!is_aligned(g, dt == TPPO_F32 ? 4 : 2) || !is_aligned(out, 2)) return TPPO_ERR_PARAM;

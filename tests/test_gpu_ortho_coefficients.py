@@ -38,3 +38,27 @@ def test_polynomials_near_zero(rows, cols, steps, coefficients):
         g = torch.from_numpy(_matrix(rng, rows, cols, kind)).float().cuda()
         worst = _error(g, steps=steps, coefficients=coefficients)
         assert worst <= NORM, (kind, worst)
+
+
+@pytest.mark.parametrize("rows,cols", [(512, 512), (700, 520), (530, 1100), (1024, 1024)])
+@pytest.mark.parametrize("steps", [6, 7, 8, 10])
+def test_more_steps_than_one_pass_allows(rows, cols, steps):
+    """Small singular values, and what rounding puts in their place, become 3.4445 times as large a step: half a step of 24 bits, in five
+    places of the norm's size (X, the product and the sum of two steps), is that many times larger in the end where there is nothing else."""
+    rng = np.random.default_rng(rows + steps)
+    for kind, most in (("rank1", NORM + 5 * 2.0 ** -24 * 3.4445 ** steps), ("geo6", NORM), ("full", NORM)):
+        g = torch.from_numpy(_matrix(rng, rows, cols, kind)).float().cuda()
+        worst = _error(g, steps=steps)
+        assert worst <= most, (kind, worst, most)
+
+
+@pytest.mark.parametrize("rows,cols", [(70, 90), (600, 640)])
+def test_iterations_that_shrink(rows, cols):
+    """Down to 2^-11 before the last step; whatever shrinks further is refused."""
+    g = torch.from_numpy(np.random.default_rng(3).normal(size=(rows, cols))).float().cuda()
+    for steps, a in ((12, 0.5), (7, 0.31), (2, 0.001), (3, -0.02)):
+        assert _error(g, steps=steps, coefficients=(a, 0.0, 0.0)) <= NORM
+        assert _error(g, steps=steps, coefficients=(a, -0.1 * a, 0.01)) <= NORM
+    for steps, a in ((14, 0.5), (24, 0.4), (2, 0.0)):
+        with pytest.raises(RuntimeError):
+            tp.tppo_orthogonalize(g, steps=steps, coefficients=(a, 0.0, 0.0))

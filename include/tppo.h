@@ -588,7 +588,8 @@ int tppo_balance_loss_backward(const void* logits, int64_t n_rows, int64_t E, in
  * rounding puts there as well, up to 3e-7 |a|^steps of the norm.
  *
  * in : g: `count` matrices [rows, cols] of type dt, row stride ld_g, stride_g
- *      elements from one to the next; 1 <= rows, cols <= 65536, 0 <= steps <= 64;
+ *      elements from one to the next; 1 <= rows, cols <= 262144 (an LM head's
+ *      vocabulary is one side), rows * cols <= 2^32; 0 <= steps <= 64;
  *      a, b, c, eps, scale finite, eps >= 0; |a|^(steps - 1) >= 2^-12 (an X that
  *      shrinks from step to step is not held).
  *      stride_g >= 0; 0 is the same matrix every time.

@@ -498,7 +498,11 @@ __global__ __launch_bounds__(kNsThreads) void ns_begin_kernel(const T* __restric
     }
 }
 
-constexpr int64_t kNsMaxSide = 65536;
+// (a vocabulary's rows among them; pieces and tiles of one matrix are numbered in 32 bits)
+constexpr int64_t kNsMaxSide = 262144, kNsMaxEntries = (int64_t)1 << 32;
+static bool ns_sides(int64_t rows, int64_t cols) {
+    return rows >= 1 && cols >= 1 && rows <= kNsMaxSide && cols <= kNsMaxSide && rows * cols <= kNsMaxEntries;
+}
 
 struct NsLayout {
     int m, n, mp, np;
@@ -711,7 +715,7 @@ static int run_ns(const T* g, int64_t count, int64_t rows, int64_t cols, int64_t
 
 extern "C" size_t tppo_orthogonalize_workspace_bytes(int64_t count, int64_t rows, int64_t cols) {
     using namespace tppo;
-    if (count < 1 || rows < 1 || cols < 1 || rows > kNsMaxSide || cols > kNsMaxSide || count > INT32_MAX / 2) return 256;
+    if (count < 1 || !ns_sides(rows, cols) || count > INT32_MAX / 2) return 256;
     return ns_layout(count, rows, cols).total;
 }
 
@@ -720,8 +724,7 @@ extern "C" int tppo_orthogonalize(const void* g, int64_t count, int64_t rows, in
                                   int64_t stride_out, void* workspace, size_t workspace_bytes, void* stream) {
     using namespace tppo;
     if (dt != TPPO_F32 && dt != TPPO_BF16) return TPPO_ERR_DTYPE;
-    if (count < 0 || count > 65535 || rows < 1 || cols < 1 || rows > kNsMaxSide || cols > kNsMaxSide || ld_g < cols || ld_out < cols)
-        return TPPO_ERR_SIZE;
+    if (count < 0 || count > 65535 || !ns_sides(rows, cols) || ld_g < cols || ld_out < cols) return TPPO_ERR_SIZE;
     if (count > 1 && (stride_g < 0 || stride_out < (rows - 1) * ld_out + cols)) return TPPO_ERR_SIZE;
     if (steps < 0 || steps > 64 || !(eps >= 0.f)) return TPPO_ERR_PARAM;
     for (float v : {a, b, c, eps, scale})

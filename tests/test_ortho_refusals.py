@@ -24,3 +24,10 @@ def test_iterations_that_shrink(call):
     assert call(steps=2, a=0.0) == P and call(steps=2, a=0.0002) == P
     assert call(steps=13, a=0.5) == W and call(steps=2, a=0.00025) == W and call(steps=64, a=0.9) == W
     assert call(steps=1, a=0.0) == W and call(steps=0, a=0.0) == W and call(steps=64, a=1.0) == W
+
+
+def test_sides(call):
+    """A vocabulary of 152064 is a side like any other; beyond 262144, or 2^32 entries, none is."""
+    assert call(rows=152064, cols=5120) == W and call(rows=5120, cols=152064) == W and call(rows=262144, cols=16384) == W
+    assert call(rows=262145) == S and call(cols=262145) == S and call(rows=262144, cols=16385) == S and call(rows=65537, cols=65536) == S
+    assert call(rows=1 << 40, cols=1 << 40) == S

@@ -288,12 +288,15 @@ __global__ __launch_bounds__(kAddThreads) void add_rows_kernel(const float* __re
     }
 }
 
-// Workgroups of the backward kernel: as many as the chip holds at once, of no fewer than four rows each (a row of partial sums is written
-// and read again for each of them, as much as one and a half to two rows are), and no more than take the same number of turns.  us, a call, 512
-// whatever the size -> so:  20000 x 3584, bf16: 112 -> 90;  16416 x 1024, fp32: 51 -> 46.
+// Workgroups of the backward kernel: as many as the chip holds at once, of no fewer than four rows each, and of two turns where a turn is a row to
+// each of four wavefronts and there are more than 384 (a row of partial sums is written and read again for each workgroup, as much as one and a
+// half to two rows are); and no more than take the same number of turns.  us, a call, one turn / two:  1001, bf16, 1025 rows: 11.0 / 11.4, 2048: 13.7 / 12.7,
+// 4096: 19.8 / 15.7;  1024, fp32, 1025: 9.6 / 11.0, 2048: 11.2 / 11.3, 4096: 19.4 / 14.3;  four turns of a workgroup a row / three:  5120, bf16, 2513:
+// 35.6 / 43.8.  512 workgroups whatever the size / so:  20000 x 3584, bf16: 112 / 90;  16416 x 1024, fp32: 51 / 46.
 constexpr int64_t kLnPartials = 1024;
 static int64_t backward_groups(int64_t M, int rows_at_once, int resident) {
-    const int64_t most = std::min<int64_t>({kLnPartials, (int64_t)256 * resident, std::max<int64_t>(256, M / 4)});
+    const int64_t few = rows_at_once > 1 ? 384 : 256, least = rows_at_once > 1 ? 2 * rows_at_once : 4;
+    const int64_t most = std::min<int64_t>({kLnPartials, (int64_t)256 * resident, std::max<int64_t>(few, (M + least - 1) / least)});
     const int64_t groups = (M + rows_at_once - 1) / rows_at_once, turns = (groups + most - 1) / most;
     return (groups + turns - 1) / turns;
 }

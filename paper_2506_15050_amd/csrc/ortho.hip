@@ -617,6 +617,15 @@ static double ns_gram_us(int mp, int np, int64_t count, int steps) {
 static bool ns_one_pass(const NsReach& r, int m, int steps, float a, float b, float c) {
     return m >= kSplitBelow && pow(fabs((double)a), steps) <= m && fabs((double)a) + fabs((double)b) + fabs((double)c) <= 24.0 * r.least;
 }
+enum NsWay { kNsPairs, kNsOnePass, kNsThreePasses };  // X X^T alone; products of X
+static NsWay ns_way(const NsLayout& L, int64_t count, int steps, float a, float b, float c) {
+    const NsReach reach = ns_reach(steps, a, b, c);
+    const bool one = ns_one_pass(reach, L.m, steps, a, b, c);
+    if (L.m < kGramBelow && (!one || ns_gram_us(L.mp, L.np, count, steps) < ns_direct_us(L.mp, L.np, count, steps)) &&
+        ns_gram_fits(reach, steps, a, b, c))
+        return kNsPairs;
+    return one ? kNsOnePass : kNsThreePasses;
+}
 template <bool SPLIT, NsMode MODE>
 static int launch_ns_tiles(NsArgs& p, int64_t count, hipStream_t s) {
     constexpr bool kAcross = MODE == kUpdate || MODE == kLast;
@@ -666,10 +675,8 @@ static int run_ns(const T* g, int64_t count, int64_t rows, int64_t cols, int64_t
     x.a = a; x.b = b; x.c = c;
     x.m = L.m; x.n = L.n; x.transposed = transposed;
     x.out = out; x.ld_out = ld_out; x.each_out = stride_out; x.scales = scales;
-    const NsReach reach = ns_reach(steps, a, b, c);
-    const bool split = !ns_one_pass(reach, L.m, steps, a, b, c);
-    if (L.m < kGramBelow && (split || ns_gram_us(L.mp, L.np, count, steps) < ns_direct_us(L.mp, L.np, count, steps)) &&
-        ns_gram_fits(reach, steps, a, b, c)) {
+    const NsWay way = ns_way(L, count, steps, a, b, c);
+    if (way == kNsPairs) {
         const NsShape shape = {L.m, L.n, L.mp, L.np, transposed, count, steps, a, b, c, out, ld_out, stride_out};
         return ns_gram(shape, hi[0], lo[0], scales, ws + L.shared, s);
     }
@@ -708,7 +715,7 @@ static int run_ns(const T* g, int64_t count, int64_t rows, int64_t cols, int64_t
         }
         return (int)TPPO_OK;
     };
-    return split ? products(std::true_type()) : products(std::false_type());
+    return way == kNsThreePasses ? products(std::true_type()) : products(std::false_type());
 }
 
 }  // namespace tppo

@@ -80,3 +80,17 @@ def test_counts_of_a_large_batch_one_apart(M, E, k, tokens):
     grad, _, own, _ = tp.tppo_balance_loss_backward(z, ids, counts_in=counts, token_denominator=tokens)
     assert own.tolist() == [M * k] + [0] * (E - 1)
     _check_nearly_even(grad, z, counts, k, tokens)
+
+
+@pytest.mark.parametrize("E,M", [(8, 500_000), (100, 77_536), (600, 60_000)])
+def test_means_over_many_rows_keep_their_digits(E, M):
+    """A workgroup adds up its rows in fp32: eight of a thread for 500 000 of 8 experts, 10 of 100 (32 rows at a time in each of 512), 15 of
+    600 (8 rows); its lanes, wavefronts and the probability itself are the other roundings."""
+    z = torch.randn(M // 4, E, device="cuda")
+    rows = torch.randint(0, M // 4, (M,), dtype=torch.int32, device="cuda")
+    ids = torch.zeros(M // 4, 1, dtype=torch.int32, device="cuda")
+    loss, _, mean_prob = tp.tppo_balance_loss(z, ids, rows=rows)
+    p = torch.softmax(z.double(), 1)[rows.long()].mean(0).cpu().numpy()
+    worst = float((np.abs(mean_prob.double().cpu().numpy() - p) / p).max() / U)
+    assert worst <= 64 + 15 + 16, worst
+    assert abs(float(loss) - E * p[0]) <= (64 + 15 + 20) * U * E * p[0]

@@ -1,5 +1,5 @@
-"""The orthogonalisation's rules (csrc/ortho_gram.hip, host side): what the iteration makes of singular values, and which coefficients
-the way by X X^T takes."""
+"""The orthogonalisation's rules (csrc/ortho.hip, ortho_gram.hip, host side): what the iteration makes of singular values, which
+coefficients the way by X X^T takes, and which way and tiles the sizes take that the GPU tests rely on."""
 import os
 import subprocess
 
@@ -66,18 +66,53 @@ int main() {
 }
 """
 
+# count, rows, cols, steps: the way (p: pairs, 1: one pass, 3: three), rows of the tiles of X X^T and of B X
+SIZES = {(1, 1024, 4096, 5): "p", (1, 1100, 1030, 5): "p", (1, 152064, 192, 5): "p", (1, 152065, 1027, 5): "p", (1, 512, 512, 5): "p",
+         (1, 2304, 2304, 5): "1 128 128", (1, 2304, 5120, 5): "1 128 192", (8, 1100, 1030, 5): "1 128 192", (8, 700, 1500, 5): "1 128 160",
+         (40, 520, 520, 5): "1 256 128", (16, 530, 700, 5): "1 128 128", (1, 4000, 4090, 5): "1 160 256", (1, 4610, 4520, 5): "1 192 192",
+         (1, 5120, 5120, 5): "1 256 256", (1, 5121, 5300, 5): "1 256 256", (1, 5300, 4900, 5): "1 256 256", (1, 152064, 2112, 5): "1 128 256",
+         (1, 300, 450, 7): "3 128 128", (1, 700, 511, 10): "3 128 128", (1, 129, 640, 7): "3 128 128", (1, 512, 512, 6): "3 128 128",
+         (1, 1024, 1024, 7): "3 128 128", (1, 2304, 2304, 6): "1 128 128", (1, 2304, 2304, 7): "3 128 128"}
+
+WAYS = r"""
+#include <cstdio>
+#include "ortho_gram.hip"
+#include "ortho.hip"
+namespace tppo { int device_compute_units() { return 256; } }
+using namespace tppo;
+int main() {
+    long count, rows, cols;
+    int steps;
+    const float a = 3.4445f, b = -4.7750f, c = 2.0315f;
+    const int tile[] = {256, 192, 160, 128};
+    for (FILE* f = fopen("SIZES", "r"); fscanf(f, "%ld %ld %ld %d", &count, &rows, &cols, &steps) == 4;) {
+        const NsLayout L = ns_layout(count, rows, cols);
+        const NsWay way = ns_way(L, count, steps, a, b, c);
+        if (way == kNsPairs) puts("p");
+        else if (way == kNsThreePasses) puts("3 128 128");
+        else printf("1 %d %d\n", tile[ns_shape<true>(L.mp, L.mp, count).shape], tile[ns_shape<false>(L.mp, L.np, count).shape]);
+    }
+}
+"""
+
 
 def _run(tmp_path, program):
     (tmp_path / "rules.hip").write_text(program)
     subprocess.run([HIPCC, "--offload-arch=gfx950", "-O1", "-std=c++17", "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops", "-I",
                     os.path.join(ROOT, "include"), "-I", os.path.join(ROOT, "paper_2506_15050_amd", "csrc"), str(tmp_path / "rules.hip"),
                     "-o", str(tmp_path / "rules")], check=True, stdout=subprocess.PIPE, stderr=subprocess.STDOUT)
-    return subprocess.run([str(tmp_path / "rules")], check=True, stdout=subprocess.PIPE, text=True).stdout.split()
+    return subprocess.run([str(tmp_path / "rules")], check=True, stdout=subprocess.PIPE, text=True).stdout
 
 
 def test_no_singular_value_passes_the_bounds(tmp_path):
-    assert _run(tmp_path, BOUNDS) == ["0", "1"]
+    assert _run(tmp_path, BOUNDS).split() == ["0", "1"]
 
 
 def test_coefficients_of_the_way_by_pairs(tmp_path):
-    assert _run(tmp_path, TAKEN) == ["1"] * 5 + ["0"] * 9
+    assert _run(tmp_path, TAKEN).split() == ["1"] * 5 + ["0"] * 9
+
+
+def test_ways_and_tiles(tmp_path):
+    (tmp_path / "sizes").write_text("\n".join(" ".join(map(str, size)) for size in SIZES))
+    got = _run(tmp_path, WAYS.replace("SIZES", str(tmp_path / "sizes"))).splitlines()
+    assert dict(zip(SIZES, got)) == SIZES

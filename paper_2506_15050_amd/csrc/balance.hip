@@ -237,6 +237,7 @@ __global__ __launch_bounds__(kBlThreads) void balance_rows_kernel(Balance b) {
             for (int i = 0; i < kPieces; ++i)
 #pragma unroll
                 for (int e = 0; e < kN; ++e) {
+                    // (the product is rounded, half a step for each unit of distance from the top, of a p that is e to the minus that)
                     z[i][e] = __builtin_amdgcn_exp2f((z[i][e] - top) * 1.4426950408889634f);
                     sum += z[i][e];
                 }

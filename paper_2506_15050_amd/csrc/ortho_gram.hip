@@ -146,7 +146,7 @@ __global__ __launch_bounds__(kPairThreads, STAGES == 2 ? 4 : 2) void ns_pair_ker
     f32x4 acc[2] = {}, cross[2] = {};
     for (int it = 0; it < STAGES - 1 && it < stages; ++it) issue(first + it, it);
     for (int it = 0; it < stages; ++it) {
-        const int behind = min(STAGES - 2, stages - 1 - it);         // stages asked for after this one, eight transfers each
+        const int behind = min(STAGES - 2, stages - 1 - it);         // stages asked for after this one, four transfers each
         if (behind == 0) __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));
         else __builtin_amdgcn_s_waitcnt(vmcnt_imm(4));
         __syncthreads();                             // this stage is there for everyone, and everyone has left the one before

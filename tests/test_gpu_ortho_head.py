@@ -24,7 +24,7 @@ def _iteration(g):
 
 
 # X X^T alone, all steps in one workgroup or by pairs, and products of X, wide and tall
-@pytest.mark.parametrize("rows,cols,dtype", [(152064, 64, torch.float32), (90, 262144, torch.bfloat16), (152064, 192, torch.float32),
+@pytest.mark.parametrize("rows,cols,dtype", [(262144, 1, torch.float32), (3, 262143, torch.float32), (152064, 64, torch.float32), (90, 262144, torch.bfloat16), (152064, 192, torch.float32),
                                              (152065, 1027, torch.bfloat16), (152064, 2112, torch.float32), (2049, 152063, torch.float32)])
 def test_a_vocabulary_of_rows(rows, cols, dtype):
     g = torch.randn(rows, cols, device="cuda")
